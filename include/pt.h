@@ -189,6 +189,140 @@ int pt_track_merge(const void* const* host_tracks, int32_t n, int64_t tokens, in
  * hip_stream.  Errors: NULL_POINTER, INVALID_ARGUMENT (rows < 0 or vocab < 1). */
 int pt_argmax(const float* dev_logits, int32_t rows, int32_t vocab, int32_t* dev_out, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Serving over a paged cache: stateless operators, no handle.  A serving program that admits and drops requests keeps
+ * keys and values in pages of a pool instead of one stretch per sequence; every step it appends the new rows' keys and
+ * values (pt_paged_append, which also applies the rotary positions), attends over them (pt_paged_attention), moves or
+ * forks pages now and then (pt_page_copy), and picks the next tokens (pt_sample).  The heads of all tracks lie side by
+ * side: a cache of a PT model has n_tracks * n_kv_heads KV heads and its queries n_tracks * n_heads heads.
+ *
+ * All device work is enqueued on the hip_stream argument (NULL = the default stream) of the current device and is
+ * asynchronous.  Nothing is allocated, nothing is kept between calls, every kernel may be captured into a HIP graph: the
+ * descriptors are read during the call, the device arrays they point to when the kernels run.  Calls that share a
+ * workspace must not overlap.
+ * ------------------------------------------------------------------------------------------------------------ */
+
+/* A pool of pages: element (layer, page, kv head, slot, c) of K lies at k + layer * layer_stride + page * page_stride +
+ * head * head_stride + slot * token_stride + c, and of V likewise from v; strides in elements, the innermost is 1.
+ *   page_size   a power of two in 16..4096: positions per page
+ *   head_dim    a multiple of 8 in 8..256
+ *   n_pages     1 or more
+ *   strides     multiples of 16 bytes, not negative; token_stride in head_dim..2^24, page_size * token_stride < 2^31.
+ *               Elements of the pool must not overlap.
+ * k and v are 16-byte aligned device pointers. */
+typedef struct pt_paged_cache {
+  void* k;
+  void* v;
+  int32_t dtype; /* PT_F32 | PT_BF16 */
+  int32_t n_layers, n_pages, page_size, n_kv_heads, head_dim;
+  int64_t layer_stride, page_stride, head_stride, token_stride;
+} pt_paged_cache;
+
+/* The rows of one step, packed sequence after sequence.  Sequence b has rows row_start[b] .. row_start[b+1]-1 (none, one,
+ * or a chunk of its prompt) and holds kv_len[b] positions once they are appended, so its row i is at position
+ * kv_len[b] - n + i with n = row_start[b+1] - row_start[b].  A row whose position is negative (n > kv_len[b]) is padding.
+ * Position p of sequence b lies in page pages[b * pages_stride + p / page_size] at slot p % page_size.
+ *   row_start  int32 [n_seqs + 1], ascending from 0 on; rows from row_start[n_seqs] on are left as they are
+ *   kv_len     int32 [n_seqs]
+ *   pages      int32 [n_seqs, pages_stride]; entries beyond a sequence's last position are not read
+ *   total_rows rows of the caller's buffers, an upper bound of row_start[n_seqs]
+ *   max_q_len, max_kv_len  upper bounds of n and kv_len (0: not known); tight ones make better launches, since
+ *              the arrays are on the device.  max_kv_len <= pages_stride * page_size
+ *   status     int32 on the device or NULL: bit 0 is raised when a page outside [0, n_pages) is met (page 0 is read in its
+ *              place, nothing is written to it), bit 1 when row_start, kv_len or their bounds contradict each other
+ *              (they are clamped).  The outputs of those sequences are meaningless; nothing outside the buffers is touched.
+ * All pointers are device pointers. */
+typedef struct pt_paged_batch {
+  const int32_t* row_start;
+  const int32_t* kv_len;
+  const int32_t* pages;
+  int64_t pages_stride;
+  int32_t n_seqs, total_rows, max_q_len, max_kv_len;
+  int32_t* status;
+} pt_paged_batch;
+
+/* Rows of heads: element (row, head, c) at data + row * row_stride + head * head_stride + c (elements).  data 16-byte
+ * aligned, both strides multiples of 16 bytes and not negative; of the cache's dtype.  A view into a fused product's
+ * output is fine. */
+typedef struct pt_head_rows {
+  void* data;
+  int64_t row_stride, head_stride;
+} pt_head_rows;
+
+/* Rotary positions.  The first rotary_dim elements of a head are r/2 pairs (a, b), r = rotary_dim: HALF pairs element j
+ * with j + r/2, INTERLEAVED 2j with 2j + 1.  At position p pair j becomes m * (a cos(p f_j) - b sin(p f_j),
+ * b cos(p f_j) + a sin(p f_j)); the other elements are copied.  f_j = theta^(-2j/r), scaled for contexts longer than
+ * the model was trained for:
+ *   LINEAR    f_j / factor
+ *   BY_PARTS  f_j * (w + (1 - w) / factor), w = clamp((original_len f_j / 2 pi - low) / (high - low), 0, 1): pairs that turn more
+ *             than `high` times over the original length keep their frequency, those below `low` turns are divided
+ * Angles are formed in 64 bits, so far positions are as exact as near ones.  Filled by pt_rope_init; turns = f_j / 2 pi. */
+enum { PT_ROPE_HALF = 0, PT_ROPE_INTERLEAVED = 1 };
+enum { PT_ROPE_UNSCALED = 0, PT_ROPE_LINEAR = 1, PT_ROPE_BY_PARTS = 2 };
+typedef struct pt_rope {
+  int32_t layout, rotary_dim;
+  double magnitude;
+  double turns[128];
+} pt_rope;
+
+/* Host only.  rotary_dim: even, 2..256; theta > 0; magnitude (m above) finite.  factor, low, high and original_len are read
+ * by the scalings that use them: factor > 0, 0 <= low < high, original_len >= 1.
+ * Errors: NULL_POINTER, INVALID_ARGUMENT. */
+int pt_rope_init(pt_rope* out, int32_t layout, int32_t rotary_dim, double theta, int32_t scaling, double factor, double low,
+                 double high, int32_t original_len, double magnitude);
+
+/* Appends the rows' keys and values to layer `layer` of the cache, and rotates queries and keys to their rows' positions on
+ * the way.  rope NULL: nothing is rotated.  k, v: rows of n_kv_heads heads.  q, q_out: rows of n_heads heads, or both NULL;
+ * q_out may be q itself (same strides) and may not overlap it otherwise.  Rows of padding store nothing in the cache
+ * (their q_out is rotated like any).  A page that receives rows must belong to one sequence of the batch only.
+ * Arithmetic in fp32 on the stored values, one rounding to the dtype.
+ * Errors: NULL_POINTER, INVALID_ARGUMENT. */
+int pt_paged_append(const pt_paged_cache* cache, int32_t layer, const pt_paged_batch* batch, const pt_rope* rope,
+                    const pt_head_rows* q, const pt_head_rows* q_out, int32_t n_heads, const pt_head_rows* k,
+                    const pt_head_rows* v, void* hip_stream);
+
+/* Attention of the batch's rows over what their sequences hold in layer `layer`, the rows' own keys included (append
+ * first).  q and out: rows of n_heads heads, a multiple of n_kv_heads; query head c uses KV head c / (n_heads / n_kv_heads).
+ *   out[row, c] = sum_j softmax_j(scale * q[row, c] . K[j]) V[j]
+ * over the positions j up to the row's own (causal != 0) or over all of its sequence's.  A row that sees nothing
+ * (padding, an empty sequence) becomes zero.  What lies in pages behind a row's last visible position, be it infinite or
+ * no number, has no influence.  Scores, statistics and sums are fp32; with a bf16 cache the probabilities are rounded to
+ * bf16 for the matrix cores.  out may be q itself (same strides).
+ *   workspace  16-byte aligned device memory of pt_paged_attention_bytes, or NULL where that is 0; needs no clearing
+ * Long sequences are cut into ranges of keys that workgroups take on their own and a second kernel joins; the result is
+ * the same from call to call.  Errors: NULL_POINTER, INVALID_ARGUMENT, ARENA_TOO_SMALL. */
+int pt_paged_attention_bytes(const pt_paged_cache* cache, const pt_paged_batch* batch, int32_t n_heads, size_t* bytes);
+int pt_paged_attention(const pt_paged_cache* cache, int32_t layer, const pt_paged_batch* batch, const pt_head_rows* q,
+                       const pt_head_rows* out, int32_t n_heads, float scale, int32_t causal, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
+/* Copies pages inside the pool, K and V of every layer: pair i copies page host_pairs[2i] to page host_pairs[2i+1]
+ * (HOST array, read during the call).  This is what forking a sequence in the middle of a page, copy-on-write and
+ * compaction need; which pages are free is the caller's bookkeeping.  No page may be written twice or be both read and
+ * written in one call (the copies run in any order).
+ * Errors: NULL_POINTER, INVALID_ARGUMENT (also: a page out of range, written twice, or both read and written). */
+int pt_page_copy(const pt_paged_cache* cache, const int32_t* host_pairs, int32_t n_pairs, void* hip_stream);
+
+/* Samples one token per row of dev_logits (fp32 [rows, vocab], row_stride elements from row to row), beside pt_argmax:
+ *   w_i  = exp((logit_i - largest logit) / temperature); a logit of -infinity or NaN has no weight
+ *   top_k  (k > 0 and k < vocab) keeps the k largest logits, of equal ones those of lowest index
+ *   top_p  (p < 1) keeps, of what is left in that order, the shortest prefix that holds at least p of the weight,
+ *          and always the first
+ *   min_p  (> 0) keeps of these the tokens with w_i >= min_p, and always the largest
+ *   out  = the first token, in order of index, at which the running sum of the kept weights exceeds uniform * their sum
+ * Parameters are device arrays of `rows` entries: uniform fp32 in [0, 1) (values outside are taken as the nearer end);
+ * temperature fp32 (0, negative or NaN: the largest logit, lowest index on ties), top_k int32, top_p fp32, min_p fp32, each of
+ * which may be NULL (temperature 1; filter off).  Weights and sums are in 64 bits and formed in an order that does not
+ * change, so equal inputs give equal tokens.  A row without any weight gives -1; where +infinity occurs, the tokens that have
+ * it share the weight equally.
+ *   vocab      1..2^24
+ *   workspace  16-byte aligned device memory of pt_sample_bytes, or NULL where that is 0; needs no clearing
+ * Errors: NULL_POINTER, INVALID_ARGUMENT, ARENA_TOO_SMALL. */
+int pt_sample_bytes(int32_t rows, int32_t vocab, size_t* bytes);
+int pt_sample(const float* dev_logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* dev_uniform,
+              const float* dev_temperature, const int32_t* dev_top_k, const float* dev_top_p, const float* dev_min_p,
+              int32_t* dev_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Optional observation point: when set (non-NULL), every merge inside pt_prefill /
  * pt_decode_step also stores the merged activation to dev_taps, fp32
  * [n_layers / block_depth, rows, d] with rows = B*S (prefill) or B (decode), and the per-track

@@ -20,6 +20,8 @@ PT_LOGITS_NONE, PT_LOGITS_LAST, PT_LOGITS_ALL = 0, 1, 2
 PT_FAMILY_GENERIC, PT_FAMILY_COUNT = 0, 4
 PT_TUNE_GEMM_TILE_CONFIG, PT_TUNE_SKINNY_PLAN, PT_TUNE_FOLD_RMSNORM, PT_TUNE_ATTN_PREFILL = 0, 1, 2, 3
 PT_PATH_AUTO, PT_PATH_GENERIC = 0, 1
+PT_ROPE_HALF, PT_ROPE_INTERLEAVED = 0, 1
+PT_ROPE_UNSCALED, PT_ROPE_LINEAR, PT_ROPE_BY_PARTS = 0, 1, 2
 PT_W_EMBED, PT_W_HEAD, PT_W_Q, PT_W_K, PT_W_V, PT_W_O, PT_W_G, PT_W_U, PT_W_D, PT_W_G1, PT_W_G2, PT_W_GF, PT_W_ROUTER = range(1, 14)
 WEIGHT_IDS = {"embed": PT_W_EMBED, "head": PT_W_HEAD, "wq": PT_W_Q, "wk": PT_W_K, "wv": PT_W_V,
               "wo": PT_W_O, "wg": PT_W_G, "wu": PT_W_U, "wd": PT_W_D, "g1": PT_W_G1, "g2": PT_W_G2,
@@ -39,7 +41,8 @@ EXPORTS = [
     "pt_prefill", "pt_decode_step", "pt_track_merge", "pt_set_taps", "pt_set_kernel_path", "pt_reset",
     "pt_merge_count", "pt_seq_len", "pt_last_error", "pt_profile_enable", "pt_profile_read",
     "pt_profile_reset", "pt_profile_paths", "pt_sync_status", "pt_set_tuning", "pt_argmax", "pt_decode_step_static", "pt_prefill_ragged", "pt_seq_lens",
-    "pt_set_moe_routes",
+    "pt_set_moe_routes", "pt_rope_init", "pt_paged_append", "pt_paged_attention_bytes", "pt_paged_attention",
+    "pt_page_copy", "pt_sample_bytes", "pt_sample",
 ]
 
 KERNEL_CLASSES = ["embed", "rmsnorm", "gemm_qkv", "attn_prefill", "attn_decode", "gemm_out",
@@ -52,6 +55,25 @@ class pt_config(C.Structure):
         "d_ffn", "vocab", "max_batch", "max_seq", "dtype")] + [
         (n, C.c_float) for n in ("merge_scale", "rms_eps", "rope_theta", "init_std")] + [
         (n, C.c_int32) for n in ("n_experts", "top_k")]
+
+
+class pt_paged_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(n, C.c_int32) for n in (
+        "dtype", "n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim")] + [(n, C.c_int64) for n in (
+            "layer_stride", "page_stride", "head_stride", "token_stride")]
+
+
+class pt_paged_batch(C.Structure):
+    _fields_ = [("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p), ("pages_stride", C.c_int64)] + [
+        (n, C.c_int32) for n in ("n_seqs", "total_rows", "max_q_len", "max_kv_len")] + [("status", C.c_void_p)]
+
+
+class pt_head_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class pt_rope(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rotary_dim", C.c_int32), ("magnitude", C.c_double), ("turns", C.c_double * 128)]
 
 
 class PTError(RuntimeError):
@@ -101,6 +123,15 @@ def lib() -> C.CDLL:
     L.pt_sync_status.argtypes = [vp]
     L.pt_set_tuning.argtypes = [i32, i32]
     L.pt_argmax.argtypes = [vp, i32, i32, vp, vp]
+    cachep, batchp, rowsp, ropep = C.POINTER(pt_paged_cache), C.POINTER(pt_paged_batch), C.POINTER(pt_head_rows), C.POINTER(pt_rope)
+    f64 = C.c_double
+    L.pt_rope_init.argtypes = [ropep, i32, i32, f64, i32, f64, f64, f64, i32, f64]
+    L.pt_paged_append.argtypes = [cachep, i32, batchp, ropep, rowsp, rowsp, i32, rowsp, rowsp, vp]
+    L.pt_paged_attention_bytes.argtypes = [cachep, batchp, i32, C.POINTER(sz)]
+    L.pt_paged_attention.argtypes = [cachep, i32, batchp, rowsp, rowsp, i32, C.c_float, i32, vp, sz, vp]
+    L.pt_page_copy.argtypes = [cachep, vp, i32, vp]
+    L.pt_sample_bytes.argtypes = [i32, i32, C.POINTER(sz)]
+    L.pt_sample.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.pt_last_error.argtypes = []
     L.pt_last_error.restype = C.c_char_p
     for name in EXPORTS:
@@ -166,6 +197,213 @@ def pt_argmax(logits, out=None, stream=None):
         out = torch.empty((logits.shape[0],), dtype=torch.int32, device=logits.device)
     st = torch.cuda.current_stream().cuda_stream if stream is None else getattr(stream, "cuda_stream", stream)
     _check(lib().pt_argmax(logits.data_ptr(), logits.shape[0], logits.shape[1], out.data_ptr(), st))
+    return out
+
+
+# -- serving over a paged cache ------------------------------------------------------------------
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise PTError(PT_ERR_INVALID_ARGUMENT, what)
+
+
+class _on:
+    """Runs a call on a tensor's device and on `stream` (None: that device's current stream)."""
+
+    def __init__(self, tensor, stream=None):
+        import torch
+        self.device, self.stream = tensor.device, stream
+        _need(self.device.type == "cuda", "the tensors must be on a GPU")
+        self.guard = None if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
+
+    def __enter__(self):
+        import torch
+        if self.guard is not None:
+            self.guard.__enter__()
+        st = torch.cuda.current_stream(self.device) if self.stream is None else self.stream
+        return getattr(st, "cuda_stream", st)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+        return False
+
+
+def _empty(shape, dtype, device, stream):
+    """A tensor for a call on `stream`, allocated on that stream, so that neither earlier nor later owners of its memory
+    overlap the call."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream, device=device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _scratch(given, nbytes: int, device, stream):
+    """(workspace, its bytes): the caller's, or one for this call."""
+    import torch
+    if given is None:
+        return (None, 0) if nbytes == 0 else (_empty(nbytes, torch.uint8, device, stream), nbytes)
+    _need(given.device == device and given.is_contiguous(), "workspace must be contiguous and on the operands' device")
+    return given, given.numel() * given.element_size()
+
+
+class PTRope:
+    """Rotary positions (pt_rope_init): layout PT_ROPE_HALF or PT_ROPE_INTERLEAVED of a head's first rotary_dim elements, base
+    theta; scaling PT_ROPE_LINEAR by `factor`, or PT_ROPE_BY_PARTS by `factor` for pairs that turn less than `low` times
+    over original_len positions, none above `high` turns and blended in between; rotated vectors are multiplied with
+    `magnitude`."""
+
+    def __init__(self, layout: int, rotary_dim: int, theta: float = 10000.0, scaling: int = PT_ROPE_UNSCALED, factor: float = 1.0,
+                 low: float = 1.0, high: float = 32.0, original_len: int = 1, magnitude: float = 1.0):
+        self.c = pt_rope()
+        _check(lib().pt_rope_init(C.byref(self.c), layout, rotary_dim, theta, scaling, factor, low, high, original_len, magnitude))
+
+
+class PTPagedCache:
+    """A pool of pages: k and v of one shape [layers, pages, kv heads, page size, head width], float32 or bfloat16, the same
+    strides, the last dimension contiguous (other orders as permuted views)."""
+
+    def __init__(self, k, v):
+        import torch
+        _need(k.dim() == 5 and k.shape == v.shape, "k and v must be [layers, pages, kv heads, page size, head width]")
+        _need(k.dtype == v.dtype and k.dtype in (torch.float32, torch.bfloat16), "k and v must both be float32 or both bfloat16")
+        _need(k.device == v.device, "k and v must be on one device")
+        # the stride of a dimension of one entry says nothing
+        st = [0 if n == 1 else s for n, s in zip(k.shape, k.stride())]
+        _need(st == [0 if n == 1 else s for n, s in zip(v.shape, v.stride())] and (st[4] == 1 or k.shape[4] == 1),
+              "k and v must have the same strides and a contiguous last dimension")
+        if k.shape[3] == 1:
+            st[3] = k.shape[4]
+        self.k, self.v = k, v
+        self.c = pt_paged_cache(k.data_ptr(), v.data_ptr(), PT_F32 if k.dtype == torch.float32 else PT_BF16, k.shape[0], k.shape[1],
+                                k.shape[3], k.shape[2], k.shape[4], st[0], st[1], st[2], st[3])
+
+
+class PTPagedBatch:
+    """The rows of one step (pt_paged_batch): int32 device tensors row_start [n + 1], kv_len [n] and pages [n, width].  Their
+    contents may change between calls (a captured graph reads them when it is replayed); the bounds hold for all of them.
+    status: int32 device tensor of one element that collects the kernels' complaints, or None."""
+
+    def __init__(self, row_start, kv_len, pages, total_rows: int, max_q_len: int = 0, max_kv_len: int = 0, status=None):
+        import torch
+        for t in (row_start, kv_len, pages) + (() if status is None else (status,)):
+            _need(t.dtype == torch.int32 and t.device == pages.device, "row_start, kv_len, pages and status must be int32 on one device")
+        _need(row_start.dim() == 1 and kv_len.dim() == 1 and pages.dim() == 2, "row_start and kv_len have one dimension, pages two")
+        n = kv_len.shape[0]
+        _need(row_start.shape[0] == n + 1 and pages.shape[0] == n, "row_start needs one entry more than kv_len, pages as many rows")
+        _need(row_start.is_contiguous() and kv_len.is_contiguous(), "row_start and kv_len must be contiguous")
+        _need(pages.shape[1] <= 1 or pages.stride(1) == 1, "the rows of pages must be contiguous")
+        _need(status is None or status.numel() >= 1, "status needs one element")
+        # with one sequence the stride between rows says nothing; rows further apart than their width hold no more entries
+        self.width = pages.shape[1]
+        _need(n <= 1 or pages.stride(0) >= self.width, "the rows of pages overlap")
+        self.row_start, self.kv_len, self.pages, self.status = row_start, kv_len, pages, status
+        self.c = pt_paged_batch(row_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), self.width if n <= 1 else pages.stride(0), n,
+                                total_rows, max_q_len, max_kv_len, _ptr(status))
+        self.given = max_kv_len
+
+    def bound(self, cache):
+        """The C descriptor with max_kv_len filled in from the table's width where it was not given."""
+        room = self.width * cache.c.page_size
+        _need(self.given <= room, "max_kv_len exceeds the page table")
+        self.c.max_kv_len = self.given or min(room, 0x7fffffff)
+        return self.c
+
+
+def _rows(t, name: str, cache, batch, heads: int = 0):
+    """pt_head_rows of a device tensor [rows, heads, head width]."""
+    _need(t.dim() == 3 and t.dtype == cache.k.dtype and t.device == cache.k.device, "%s must be [rows, heads, width] of the cache's type and device" % name)
+    _need(t.shape[0] >= batch.c.total_rows and t.shape[2] == cache.c.head_dim, "%s is too small or of another head width" % name)
+    _need(heads == 0 or t.shape[1] == heads, "%s has %d heads, not %d" % (name, t.shape[1], heads))
+    _need(t.stride(2) == 1, "the last dimension of %s must be contiguous" % name)
+    st = t.stride()
+    return pt_head_rows(t.data_ptr(), 0 if t.shape[0] == 1 else st[0], 0 if t.shape[1] == 1 else st[1])
+
+
+def pt_paged_append(cache: PTPagedCache, layer: int, batch: PTPagedBatch, k, v, q=None, q_out=None, rope: Optional[PTRope] = None, stream=None):
+    """Stores the batch's keys and values [rows, kv heads, width] in their pages, queries and keys rotated on the way.
+    q [rows, heads, width] goes to q_out (made if not given; may be q).  Returns q_out."""
+    kv = cache.c.n_kv_heads
+    cb = batch.bound(cache)
+    _need(batch.pages.device == cache.k.device, "batch and cache must be on one device")
+    ck, cv = _rows(k, "k", cache, batch, kv), _rows(v, "v", cache, batch, kv)
+    with _on(cache.k, stream) as st:
+        cq = co = None
+        heads = 0
+        if q is not None:
+            heads = q.shape[1]
+            if q_out is None:
+                q_out = _empty(q.shape, q.dtype, q.device, stream)
+            cq, co = _rows(q, "q", cache, batch), _rows(q_out, "q_out", cache, batch, heads)
+        else:
+            _need(q_out is None, "q_out without q")
+        _check(lib().pt_paged_append(cache.c, layer, cb, None if rope is None else rope.c, cq, co, heads, ck, cv, st))
+    return q_out
+
+
+def pt_paged_attention_bytes(cache: PTPagedCache, batch: PTPagedBatch, n_heads: int) -> int:
+    """Workspace bytes of pt_paged_attention."""
+    n = C.c_size_t()
+    _check(lib().pt_paged_attention_bytes(cache.c, batch.bound(cache), n_heads, C.byref(n)))
+    return n.value
+
+
+def pt_paged_attention(cache: PTPagedCache, layer: int, batch: PTPagedBatch, q, out=None, scale: Optional[float] = None, causal: bool = True,
+                       workspace=None, stream=None):
+    """Attention of the batch's queries [rows, heads, width] over their sequences' pages.  scale: 1 / sqrt(width) if not
+    given.  workspace: uint8 device tensor of pt_paged_attention_bytes (made per call if not given).  Returns out."""
+    cb = batch.bound(cache)
+    _need(batch.pages.device == cache.k.device, "batch and cache must be on one device")
+    cq = _rows(q, "q", cache, batch)
+    heads = q.shape[1]
+    with _on(cache.k, stream) as st:
+        if out is None:
+            out = _empty(q.shape, q.dtype, q.device, stream)
+        co = _rows(out, "out", cache, batch, heads)
+        ws, size = _scratch(workspace, 0 if workspace is not None else pt_paged_attention_bytes(cache, batch, heads), q.device, stream)
+        _check(lib().pt_paged_attention(cache.c, layer, cb, cq, co, heads, q.shape[2] ** -0.5 if scale is None else scale, int(causal),
+                                        _ptr(ws), size, st))
+    return out
+
+
+def pt_page_copy(cache: PTPagedCache, pairs, stream=None) -> None:
+    """Copies pages inside the cache, every layer, K and V.  pairs: host array or list of (from, to)."""
+    p = np.asarray(pairs)
+    if p.size == 0:
+        return
+    _need(p.ndim == 2 and p.shape[1] == 2 and p.dtype.kind in "iu", "pairs must be whole numbers [n, 2]")
+    if p.dtype != np.int32:
+        _need(int(p.min()) >= 0 and int(p.max()) < 2 ** 31, "a page out of range")
+    p = np.ascontiguousarray(p, dtype=np.int32)
+    with _on(cache.k, stream) as st:
+        _check(lib().pt_page_copy(cache.c, p.ctypes.data, p.shape[0], st))
+
+
+def pt_sample_bytes(rows: int, vocab: int) -> int:
+    """Workspace bytes of pt_sample."""
+    n = C.c_size_t()
+    _check(lib().pt_sample_bytes(rows, vocab, C.byref(n)))
+    return n.value
+
+
+def pt_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, out=None, workspace=None, stream=None):
+    """One token per row of logits (float32 device tensor [rows, vocab], rows contiguous) by the given uniform numbers [rows]
+    in [0, 1).  temperature, top_p, min_p: float32 [rows], top_k: int32 [rows], or None.  Returns int32 [rows]."""
+    import torch
+    _need(logits.dim() == 2 and logits.dtype == torch.float32 and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits must be float32 [rows, vocab] with contiguous rows")
+    rows, vocab = logits.shape
+    for t, ty, name in ((uniform, torch.float32, "uniform"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (out, torch.int32, "out")):
+        if t is not None or name == "uniform":
+            _need(t is not None and t.dtype == ty and t.shape == (rows,) and t.device == logits.device and (rows <= 1 or t.stride(0) == 1),
+                  "%s must be contiguous %s [rows] on the logits' device" % (name, str(ty)[6:]))
+    with _on(logits, stream) as st:
+        if out is None:
+            out = _empty((rows,), torch.int32, logits.device, stream)
+        ws, size = _scratch(workspace, 0 if workspace is not None else pt_sample_bytes(rows, vocab), logits.device, stream)
+        _check(lib().pt_sample(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab, uniform.data_ptr(), _ptr(temperature), _ptr(top_k),
+                               _ptr(top_p), _ptr(min_p), out.data_ptr(), _ptr(ws), size, st))
     return out
 
 

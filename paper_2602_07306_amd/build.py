@@ -43,6 +43,10 @@ SOURCES = [
     "kernels_attn_prefill_mfma.hip",
     "kernels_attn_decode.hip",
     "kernels_moe.hip",
+    "pt_serving.cpp",
+    "kernels_paged_cache.hip",
+    "kernels_paged_attn.hip",
+    "kernels_sample.hip",
 ]
 
 COMMON = [

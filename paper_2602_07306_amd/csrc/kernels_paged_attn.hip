@@ -1,0 +1,615 @@
+// Attention of a step's rows over a paged cache: o = softmax(scale q K^T) V per row and head, over the positions that the
+// row may see.  One pass over the keys with a running maximum and sum.
+//
+// Rows of a sequence that share a KV head - its n new rows times the G query heads of the group - are packed into tiles:
+// packed row r is new row r / G, head r % G of the group.  A workgroup takes one tile, one KV head and one range of keys; its
+// four wavefronts take the range's key tiles in turn and are merged at the end through LDS.  Where one range does not hold all
+// keys, each leaves its unscaled sums and statistics to paged_combine_kernel.
+#include <algorithm>
+
+#include "pt_paged_device.h"
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void* lptr_t;
+typedef __attribute__((address_space(3))) s16x4_t* lptr4_t;
+typedef const __attribute__((address_space(1))) void* gptr_t;
+
+constexpr int PA_MAX_SPLITS = 64;   // a wavefront of the combine holds one range's statistics per lane
+
+// A tile of packed rows: its sequence, its rows, the keys that its last row sees, and in how many ranges they are cut.
+struct paged_tile {
+  paged_seq sq;
+  int seq, row0, nrows, base_pos, vis, nsplit;
+};
+
+__device__ __forceinline__ int paged_vis(const pt_paged_attn_args& a, const paged_seq& sq, int last_row) {
+  const int pos = sq.kv - sq.n + last_row;
+  return pos < 0 ? 0 : a.causal ? pos + 1 : sq.kv;
+}
+
+// Tile `tile` of the batch; false where there are fewer.  Sequences are scanned 64 at a time (wavefront-uniform result).
+__device__ __forceinline__ bool paged_find_tile(const pt_paged_attn_args& a, int tile, paged_tile* t) {
+  const int G = a.H / a.Hkv, lane = threadIdx.x & 63;
+  int seq = tile, in_seq = 0;
+  if (a.b.max_q_len * (int64_t)G > a.tile_rows) {   // more than one tile per sequence is possible
+    int before = 0;
+    seq = -1;
+    for (int base = 0; base < a.b.n_seqs; base += 64) {
+      int n = 0;
+      if (base + lane < a.b.n_seqs) {
+        const int r0 = a.b.row_start[base + lane], r1 = a.b.row_start[base + lane + 1];
+        const int first = min(max(r0, 0), a.b.total_rows);
+        const int rows = min(min(max(r1, first), a.b.total_rows) - first, a.b.max_q_len);
+        n = (int)(((int64_t)rows * G + a.tile_rows - 1) / a.tile_rows);
+      }
+      int sum = n;   // inclusive over the lanes
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += up;
+      }
+      const uint64_t past = __ballot(before + sum > tile);
+      if (past) {
+        const int l = __ffsll((unsigned long long)past) - 1;
+        seq = base + l;
+        in_seq = tile - before - (__shfl(sum, l, 64) - __shfl(n, l, 64));
+        break;
+      }
+      before += __shfl(sum, 63, 64);
+    }
+    if (seq < 0) return false;
+  }
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  in_seq = __builtin_amdgcn_readfirstlane(in_seq);
+  t->seq = seq;
+  t->sq = paged_load_seq(a.b, seq);
+  t->row0 = in_seq * a.tile_rows;
+  t->nrows = (int)min((int64_t)a.tile_rows, (int64_t)t->sq.n * G - t->row0);
+  if (t->nrows <= 0) return false;
+  t->base_pos = t->sq.kv - t->sq.n;
+  t->vis = paged_vis(a, t->sq, (t->row0 + t->nrows - 1) / G);
+  t->nsplit = max(1, (int)(((int64_t)t->vis + a.chunk - 1) / a.chunk));
+  return true;
+}
+
+// One row by one wavefront, keys k0 .. k1-1, touching no other key: lane = key for the scores, lane = element for the values.
+// For rows whose tile met an infinity or a NaN: a key that the mask drops still enters the tile's product, as 0 * V.
+template <typename T>
+__device__ __forceinline__ void paged_row_alone(const pt_paged_attn_args& a, const T* q, const T* K, const T* V, const int32_t* pages, int k0, int k1,
+                                             float* m_out, float* l_out, float acc[4]) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc[i] = 0.f;
+  for (int base = k0; base < k1; base += 64) {
+    const int key = base + lane;
+    int64_t off = 0;
+    float s = -INFINITY;
+    if (key < k1) {
+      off = paged_checked(a.b, pages[key >> a.b.page_shift]) * a.page_stride + (key & ((1 << a.b.page_shift) - 1)) * a.token_stride;
+      float dot = 0.f;
+#pragma unroll 4
+      for (int e = 0; e < a.hd; ++e) dot = fmaf(elem<T>::ld(q + e) * a.q_sign, elem<T>::ld(K + off + e), dot);
+      s = dot * a.scale_log2;
+    }
+    const float m_new = fmaxf(m, wave_max(s));
+    const float ref = m_new == -INFINITY ? 0.f : m_new;
+    const float corr = __builtin_amdgcn_exp2f(m - ref);
+    const float p = key < k1 ? __builtin_amdgcn_exp2f(s - ref) : 0.f;
+    l = l * corr + wave_sum(p);
+    m = m_new;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] *= corr;
+    const int nk = min(64, k1 - base);
+    for (int kk = 0; kk < nk; ++kk) {
+      const float pk = __shfl(p, kk, 64);
+      const int64_t o = __shfl((long long)off, kk, 64);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (lane + 64 * i < a.hd) acc[i] = fmaf(pk, elem<T>::ld(V + o + lane + 64 * i), acc[i]);
+    }
+  }
+  *m_out = m;
+  *l_out = l;
+}
+
+// Result of one row over one range: the output itself, or a partial for the combine.
+template <typename T>
+__device__ __forceinline__ void paged_store_row(const pt_paged_attn_args& a, const paged_tile& t, int split, int row, int head, int lim, float m, float l, float o, int e) {
+  if (t.nsplit == 1) {
+    // sees nothing: zero; sees only scores of -infinity: 0 / 0
+    elem<T>::st((T*)a.o + row * a.o_rs + head * a.o_hs + e, lim <= 0 ? 0.f : o / l);
+  } else {
+    const int64_t at = ((int64_t)split * a.b.total_rows + row) * a.H + head;
+    a.part_o[at * a.hd + e] = o;
+    if (e == 0) a.part_ml[at] = make_float2(m, l);
+  }
+}
+
+// Merge of the four wavefronts of a workgroup: red_o [4][R][HD + 4] unscaled sums, red_ml [4][R] statistics.
+template <typename T, int HD>
+__device__ __forceinline__ void paged_merge(const pt_paged_attn_args& a, const paged_tile& t, int split, int kvh, int k0, int k1,
+                                            const float* red_o, const float2* red_ml) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, G = a.H / a.Hkv;
+  constexpr int PER = HD / 64;
+  for (int r = wave; r < t.nrows; r += 4) {
+    const int i = (t.row0 + r) / G, hh = (t.row0 + r) - i * G;
+    const int row = t.sq.first + i, head = kvh * G + hh;
+    const int lim = paged_vis(a, t.sq, i);
+    float m = -INFINITY, l = 0.f, f[4], o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, red_ml[w * a.tile_rows + r].x);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float2 ml = red_ml[w * a.tile_rows + r];
+      f[w] = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+      l += f[w] * ml.y;
+    }
+    bool odd = !(fabsf(l) < INFINITY);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) o[j] += f[w] * red_o[(w * a.tile_rows + r) * (HD + 4) + lane + 64 * j];
+      if (lane + 64 * j < a.hd) odd |= !(fabsf(o[j]) < INFINITY);
+    }
+    if (__any(odd)) {
+      const int64_t hoff = (int64_t)kvh * a.head_stride;
+      paged_row_alone<T>(a, (const T*)a.q + row * a.q_rs + head * a.q_hs, (const T*)a.kc + hoff, (const T*)a.vc + hoff,
+                         a.b.pages + t.seq * a.b.pages_stride, k0, min(k1, lim), &m, &l, o);
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (lane + 64 * j < a.hd) paged_store_row<T>(a, t, split, row, head, lim, m, l, o[j], lane + 64 * j);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// bf16.  S^T = K Q^T and O^T = V^T P^T on 16x16x32 MFMAs, so that a query is a lane (lane % 16) of both results and the
+// statistics are per lane.  A wavefront's key tile goes straight into its own LDS, K and V as they lie in their pages, 16-byte
+// chunks swizzled by row; nothing but the merge waits for another wavefront.  V^T fragments come from the transposing LDS read
+// (16 lanes read a 4 x 16 block and receive its columns).
+// MFMA contraction order of the second product: lane group g holds, of 32 keys, 4g..4g+3 of the first and of the second
+// 16 - what the S^T result leaves in its registers, and what two transposing reads deliver.
+// NQ: blocks of 16 packed rows.  FULL: hd == HD; otherwise the rest of the LDS rows is zeroed once and never loaded.
+// ------------------------------------------------------------------------------------------------
+template <int HD>
+struct paged_geom {
+  static constexpr int TK = HD == 256 ? 32 : 64;      // keys of a tile
+  static constexpr int ROWB = HD * 2, CH = HD / 8;    // bytes and 16-byte chunks of a row
+  static constexpr int RPI = 64 / CH;                 // rows per load instruction of 1024 bytes
+  static constexpr int PER16 = 16 / RPI;              // load instructions per 16 keys
+  static constexpr int TILE_B = TK * ROWB;
+  static __device__ __forceinline__ int swz(int row) { return HD == 64 ? (row >> 1) & 7 : row & 15; }
+};
+
+template <int HD, int NQ, bool FULL>
+__global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_args a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  using geo = paged_geom<HD>;
+  constexpr int TK = geo::TK, CH = geo::CH, RPI = geo::RPI, PER16 = geo::PER16, TILE_B = geo::TILE_B;
+  constexpr int NB = TK / 16, KS = HD / 32, HB = HD / 16, NU = TK / 32;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % a.Hkv;
+  const int rest = blockIdx.x / a.Hkv;
+  const int split = rest / a.tiles;
+  paged_tile t;
+  if (!paged_find_tile(a, rest - split * a.tiles, &t) || split >= t.nsplit) return;
+  const int k0 = split * a.chunk, k1 = min(t.vis, k0 + a.chunk);
+  const int G = a.H / a.Hkv;
+
+  // queries: B operand of S^T, and each one's first key that it does not see
+  bf16x8_t qf[NQ][KS];
+  int lim[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = t.row0 + n * 16 + l16, i = r / G, hh = r - i * G;
+    const bool real = n * 16 + l16 < t.nrows;
+    lim[n] = real ? min(paged_vis(a, t.sq, i), k1) : 0;
+    const bf16_t* q = (const bf16_t*)a.q + (t.sq.first + i) * a.q_rs + (kvh * G + hh) * a.q_hs;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (real && (FULL || kk * 32 + g * 8 < a.hd)) w = *(const uint4*)(q + kk * 32 + g * 8);
+      if (a.q_sign != 1.0f) {
+        const uint32_t keep = a.q_sign == 0.0f ? 0u : 0xffffffffu, flip = a.q_sign < 0.0f ? 0x80008000u : 0u;
+        w.x = (w.x & keep) ^ flip; w.y = (w.y & keep) ^ flip; w.z = (w.z & keep) ^ flip; w.w = (w.w & keep) ^ flip;
+      }
+      qf[n][kk] = *(const bf16x8_t*)&w;
+    }
+  }
+  const int lim_first = min(paged_vis(a, t.sq, t.row0 / G), k1);   // the row that sees least
+
+  char* kt = smem + wave * 2 * TILE_B;
+  char* vt = kt + TILE_B;
+  const uint32_t kt_lds = (uint32_t)(uintptr_t)(lptr_t)kt, vt_lds = kt_lds + TILE_B;
+  if (!FULL)
+    for (int i = lane; i < 2 * TILE_B / 16; i += 64) ((uint4*)kt)[i] = make_uint4(0, 0, 0, 0);
+  // a lane's source within 16 keys: its row and swizzled chunk, per load instruction
+  uint32_t voff[PER16];
+  bool on[PER16];
+#pragma unroll
+  for (int i = 0; i < PER16; ++i) {
+    const int row = i * RPI + lane / CH, c = (lane % CH) ^ geo::swz(row);
+    voff[i] = (uint32_t)(row * a.token_stride * 2 + c * 16);
+    on[i] = FULL || c * 8 < a.hd;
+  }
+  const int32_t* pages = a.b.pages + t.seq * a.b.pages_stride;
+  const int mask = (1 << a.b.page_shift) - 1;
+  // lane j: page of the tile's j-th 16 keys (of the last key in the range where those are behind it)
+  auto page_ids = [&](int kb) { return pages[min(kb + 16 * (lane & (NB - 1)), k1 - 1) >> a.b.page_shift]; };
+  auto load_tile = [&](const void* cache, uint32_t lds, int kb, int pid) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int page = paged_checked(a.b, __builtin_amdgcn_readlane(pid, j));
+      const char* base = (const char*)cache + (page * a.page_stride + ((kb + 16 * j) & mask) * a.token_stride + kvh * a.head_stride) * 2;
+#pragma unroll
+      for (int i = 0; i < PER16; ++i)
+        if (on[i])
+          __builtin_amdgcn_global_load_lds((gptr_t)(base + voff[i]), (lptr_t)(uintptr_t)(lds + (j * PER16 + i) * 1024), 16, 0, 0);
+    }
+  };
+
+  f32x4_t acc[NQ][HB];
+  float m_run[NQ], l_run[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    m_run[n] = -INFINITY;
+    l_run[n] = 0.f;
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) acc[n][hb] = {0.f, 0.f, 0.f, 0.f};
+  }
+  const float c_log2 = a.scale_log2;
+  int kb = k0 + wave * TK;
+  int pid = 0;
+  if (!FULL) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the zeros are in LDS
+  if (kb < k1) {
+    pid = page_ids(kb);
+    load_tile(a.kc, kt_lds, kb, pid);
+    load_tile(a.vc, vt_lds, kb, pid);
+    pid = page_ids(min(kb + 4 * TK, k1 - 1));
+  }
+  for (; kb < k1; kb += 4 * TK) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the tile has landed; the wavefront is alone with it
+    const bool more = kb + 4 * TK < k1, tail = kb + TK > k1;
+    bf16x8_t kf[NB][KS];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const int row = b * 16 + l16;
+        kf[b][kk] = *(const bf16x8_t*)(kt + row * geo::ROWB + (((kk * 4 + g) ^ geo::swz(row)) * 16));
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) load_tile(a.kc, kt_lds, kb + 4 * TK, pid);
+    f32x4_t s[NQ][NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        s[n][b] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[b][kk], qf[n][kk], s[n][b], 0, 0, 0);
+      }
+    union v_frag {
+      s16x4_t h[2];
+      uint32_t u[4];
+      bf16x8_t v;
+    } vf[HB][NU];
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int row = 32 * u + 16 * x + 4 * g + (l16 >> 2), c = hb * 2 + ((l16 & 3) >> 1);
+          vf[hb][u].h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr4_t)(uintptr_t)(vt_lds + row * geo::ROWB + ((c ^ geo::swz(row)) * 16) + (l16 & 1) * 8));
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) {
+      load_tile(a.vc, vt_lds, kb + 4 * TK, pid);
+      pid = page_ids(min(kb + 8 * TK, k1 - 1));
+    }
+    if (tail) {   // cache bytes behind the range are not data: zeroed, so that 0 * x stays 0
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = kb + 32 * u + 16 * (j >> 1) + 4 * g + 2 * (j & 1);
+          const uint32_t keep = (key < k1 ? 0xffffu : 0u) | (key + 1 < k1 ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb) vf[hb][u].u[j] &= keep;
+        }
+    }
+    // s[n][b], register v: key kb + 16 b + 4 g + v, query n * 16 + l16
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      if (kb + TK > lim_first) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (kb + 16 * b + 4 * g + v >= lim[n]) s[n][b][v] = -INFINITY;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[n][b][v]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float m_new = fmaxf(m_run[n], mx);
+      const float ref = m_new == -INFINITY ? 0.f : m_new;   // no key seen yet
+      const float corr = __builtin_amdgcn_exp2f((m_run[n] - ref) * c_log2);
+      const float mc = ref * c_log2;
+      float psum = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          s[n][b][v] = __builtin_amdgcn_exp2f(fmaf(s[n][b][v], c_log2, -mc));
+          psum += s[n][b][v];
+        }
+      l_run[n] = l_run[n] * corr + psum;
+      m_run[n] = m_new;
+      if (__any(corr != 1.0f)) {
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb) acc[n][hb] *= corr;
+      }
+      union {
+        uint32_t u[4];
+        bf16x8_t v;
+      } pf[NU];
+#pragma unroll
+      for (int u = 0; u < NU; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pf[u].u[j] = pack_bf16x2(s[n][2 * u + (j >> 1)][2 * (j & 1)], s[n][2 * u + (j >> 1)][2 * (j & 1) + 1]);
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int u = 0; u < NU; ++u) acc[n][hb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[hb][u].v, pf[u].v, acc[n][hb], 0, 0, 0);
+    }
+  }
+  // merge: the tiles' LDS is free once every wavefront is here
+  __syncthreads();
+  float* red_o = (float*)smem;                                      // [4][16 NQ][HD + 4]
+  float2* red_ml = (float2*)(red_o + 4 * 16 * NQ * (HD + 4));       // [4][16 NQ]
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    l_run[n] += __shfl_xor(l_run[n], 16, 64);
+    l_run[n] += __shfl_xor(l_run[n], 32, 64);
+    const int at = (wave * NQ + n) * 16 + l16;
+    if (g == 0) red_ml[at] = make_float2(m_run[n] * c_log2, l_run[n]);
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) *(f32x4_t*)(red_o + at * (HD + 4) + hb * 16 + 4 * g) = acc[n][hb];
+  }
+  __syncthreads();
+  paged_merge<bf16_t, HD>(a, t, split, kvh, k0, k1, red_o, red_ml);
+#endif
+}
+
+// ------------------------------------------------------------------------------------------------
+// fp32, on 16x16x4 MFMAs: 16 packed rows per workgroup, 16 keys per wavefront and step, operands straight from the pages.
+// The contraction over the head takes elements 16 j + 4 g + i in step (j, i), so that a lane's operands are 16-byte loads; the
+// second product's rows are head elements 64 hb + 4 r + j for the same reason.
+// ------------------------------------------------------------------------------------------------
+template <int HD>
+__global__ void __launch_bounds__(256, 1) paged_attn_f32_kernel(const pt_paged_attn_args a) {
+  constexpr int KJ = HD / 16, VH = HD / 64;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % a.Hkv;
+  const int rest = blockIdx.x / a.Hkv;
+  const int split = rest / a.tiles;
+  paged_tile t;
+  if (!paged_find_tile(a, rest - split * a.tiles, &t) || split >= t.nsplit) return;
+  const int k0 = split * a.chunk, k1 = min(t.vis, k0 + a.chunk);
+  const int G = a.H / a.Hkv;
+  f32x4_t qf[KJ];
+  const int r = t.row0 + l16, qi = r / G, hh = r - qi * G;
+  const bool real = l16 < t.nrows;
+  const int lim = real ? min(paged_vis(a, t.sq, qi), k1) : 0;
+  {
+    const float* q = (const float*)a.q + (t.sq.first + qi) * a.q_rs + (kvh * G + hh) * a.q_hs;
+#pragma unroll
+    for (int j = 0; j < KJ; ++j) {
+      qf[j] = {0.f, 0.f, 0.f, 0.f};
+      if (real && 16 * j + 4 * g < a.hd) qf[j] = *(const f32x4_t*)(q + 16 * j + 4 * g) * a.q_sign;
+    }
+  }
+  const int lim_first = min(paged_vis(a, t.sq, t.row0 / G), k1);
+  const int32_t* pages = a.b.pages + t.seq * a.b.pages_stride;
+  const int mask = (1 << a.b.page_shift) - 1;
+  f32x4_t kf[KJ], vf[VH][4];
+  auto load = [&](int kb) {   // a row behind the range is inside its page and unused: zeros for the values
+    const int page = paged_checked(a.b, pages[kb >> a.b.page_shift]);
+    const int64_t off = page * a.page_stride + (kb & mask) * a.token_stride + kvh * a.head_stride;
+    const float* k = (const float*)a.kc + off + l16 * a.token_stride + 4 * g;
+    const float* v = (const float*)a.vc + off + 4 * l16;
+#pragma unroll
+    for (int j = 0; j < KJ; ++j) {
+      kf[j] = {0.f, 0.f, 0.f, 0.f};
+      if (16 * j + 4 * g < a.hd) kf[j] = *(const f32x4_t*)(k + 16 * j);
+    }
+#pragma unroll
+    for (int h = 0; h < VH; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        vf[h][i] = {0.f, 0.f, 0.f, 0.f};
+        if (64 * h + 4 * l16 < a.hd && kb + 4 * g + i < k1) vf[h][i] = *(const f32x4_t*)(v + (4 * g + i) * a.token_stride + 64 * h);
+      }
+  };
+  f32x4_t acc[VH][4];
+#pragma unroll
+  for (int h = 0; h < VH; ++h)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[h][j] = {0.f, 0.f, 0.f, 0.f};
+  float m_run = -INFINITY, l_run = 0.f;
+  const float c_log2 = a.scale_log2;
+  int kb = k0 + wave * 16;
+  if (kb < k1) load(kb);
+  for (; kb < k1; kb += 64) {
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < KJ; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[j][i], qf[j][i], s, 0, 0, 0);
+    f32x4_t vc[VH][4];
+#pragma unroll
+    for (int h = 0; h < VH; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vc[h][i] = vf[h][i];
+    if (kb + 64 < k1) load(kb + 64);
+    if (kb + 16 > lim_first) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        if (kb + 4 * g + v >= lim) s[v] = -INFINITY;
+    }
+    float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(m_run, mx);
+    const float ref = m_new == -INFINITY ? 0.f : m_new;
+    const float corr = __builtin_amdgcn_exp2f((m_run - ref) * c_log2);
+    const float mc = ref * c_log2;
+    float psum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c_log2, -mc));
+      psum += s[v];
+    }
+    l_run = l_run * corr + psum;
+    m_run = m_new;
+#pragma unroll
+    for (int h = 0; h < VH; ++h)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[h][j] *= corr;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[h][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vc[h][i][j], s[i], acc[h][j], 0, 0, 0);
+      }
+  }
+  float* red_o = (float*)smem;
+  float2* red_ml = (float2*)(red_o + 4 * 16 * (HD + 4));
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+  const int at = wave * 16 + l16;
+  if (g == 0) red_ml[at] = make_float2(m_run * c_log2, l_run);
+#pragma unroll
+  for (int h = 0; h < VH; ++h)   // acc[h][j], register v: element 64 h + 16 g + 4 v + j
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const f32x4_t o = {acc[h][0][v], acc[h][1][v], acc[h][2][v], acc[h][3][v]};
+      *(f32x4_t*)(red_o + at * (HD + 4) + 64 * h + 16 * g + 4 * v) = o;
+    }
+  __syncthreads();
+  paged_merge<float, HD>(a, t, split, kvh, k0, k1, red_o, red_ml);
+}
+
+// Joins the ranges of one (row, head) per wavefront, in their order.  Rows whose keys fitted one range are done already.
+template <typename T>
+__global__ void __launch_bounds__(256) paged_combine_kernel(const pt_paged_attn_args a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int row = __builtin_amdgcn_readfirstlane((int)(unit / a.H)), head = __builtin_amdgcn_readfirstlane((int)(unit % a.H));
+  if (row >= a.b.total_rows) return;
+  const int seq = paged_find_row(a.b, row);
+  if (seq >= a.b.n_seqs) return;
+  const paged_seq sq = paged_load_seq(a.b, seq);
+  if (row < sq.first || row >= sq.first + sq.n) return;
+  const int G = a.H / a.Hkv;
+  const int i = row - sq.first;
+  const int tile = (i * G + head % G) / a.tile_rows;
+  const int64_t last = min((int64_t)(tile + 1) * a.tile_rows, (int64_t)sq.n * G) - 1;
+  const int nsplit = (int)(((int64_t)paged_vis(a, sq, (int)(last / G)) + a.chunk - 1) / a.chunk);
+  if (nsplit <= 1) return;
+  const int64_t step = (int64_t)a.b.total_rows * a.H, at = (int64_t)row * a.H + head;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < nsplit) ml = a.part_ml[lane * step + at];
+  const float m = wave_max(ml.x);
+  const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+  const float l = wave_sum(f * ml.y);
+  const int lim = paged_vis(a, sq, i);
+  for (int e = lane; e < a.hd; e += 64) {
+    float o = 0.f;
+    for (int s = 0; s < nsplit; ++s) o += __shfl(f, s, 64) * a.part_o[(s * step + at) * a.hd + e];
+    elem<T>::st((T*)a.o + row * a.o_rs + head * a.o_hs + e, lim <= 0 ? 0.f : o / l);
+  }
+}
+
+static int paged_blocks(int32_t dtype, int32_t hd, int64_t rows_max) {   // blocks of 16 packed rows per tile
+  if (dtype == PT_F32 || rows_max <= 16) return 1;
+  return rows_max <= 32 || hd > 128 ? 2 : 4;
+}
+
+int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const pt_paged_rows& b, pt_paged_plan* p) {
+  const int64_t G = H / Hkv, rows_max = b.max_q_len * G;
+  if (rows_max > 0x3fffffff) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "max_q_len times the heads of a group is too large");
+  p->tile_rows = 16 * paged_blocks(dtype, hd, rows_max);
+  int64_t tiles = b.n_seqs;
+  if (rows_max > p->tile_rows)
+    tiles = std::min(b.n_seqs * ((rows_max + p->tile_rows - 1) / p->tile_rows), b.total_rows * G / p->tile_rows + b.n_seqs);
+  const int64_t units = tiles * Hkv;
+  // enough ranges for 2048 workgroups, each of at least a tile for every wavefront
+  int64_t splits = std::min<int64_t>((2048 + units - 1) / units, PA_MAX_SPLITS);
+  int64_t chunk = (std::max(b.max_kv_len, 1) + splits - 1) / splits;
+  chunk = (chunk + 255) / 256 * 256;
+  splits = (std::max(b.max_kv_len, 1) + chunk - 1) / chunk;
+  if (units * splits > 0x7fffffff || (int64_t)b.total_rows * H > ((int64_t)1 << 32)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
+  p->tiles = (int32_t)tiles;
+  p->chunk = (int32_t)chunk;
+  p->n_splits = (int32_t)splits;
+  if (splits > 1) {
+    const size_t parts = (size_t)splits * b.total_rows * H;
+    p->off_ml = (parts * hd * 4 + 15) / 16 * 16;
+    p->bytes = p->off_ml + parts * 8;
+  }
+  return PT_OK;
+}
+
+template <int HD, int NQ, bool FULL>
+static int launch_paged(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
+  constexpr int LDS = std::max(8 * paged_geom<HD>::TILE_B, 4 * 16 * NQ * ((HD + 4) * 4 + 8));
+  static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
+  auto kern = paged_attn_kernel<HD, NQ, FULL>;
+  PT_SET_MAX_LDS_ONCE(kern, LDS);
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), LDS, s, a);
+  return PT_OK;
+}
+template <int HD, int NQ>
+static int launch_paged_full(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
+  return a.hd == HD ? launch_paged<HD, NQ, true>(a, grid, s) : launch_paged<HD, NQ, false>(a, grid, s);
+}
+template <int HD>
+static int launch_paged_f32(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
+  hipLaunchKernelGGL(paged_attn_f32_kernel<HD>, dim3(grid), dim3(256), 4 * 16 * ((HD + 4) * 4 + 8), s, a);
+  return PT_OK;
+}
+
+int pt_launch_paged_attn(const pt_paged_attn_args& a, int32_t dtype, hipStream_t s) {
+  const unsigned grid = (unsigned)((int64_t)a.tiles * a.Hkv * a.n_splits);
+  const int nq = a.tile_rows / 16;
+  int rc;
+  if (dtype == PT_F32) {
+    rc = a.hd <= 64 ? launch_paged_f32<64>(a, grid, s) : a.hd <= 128 ? launch_paged_f32<128>(a, grid, s) : launch_paged_f32<256>(a, grid, s);
+  } else if (a.hd <= 64) {
+    rc = nq == 1 ? launch_paged_full<64, 1>(a, grid, s) : nq == 2 ? launch_paged_full<64, 2>(a, grid, s) : launch_paged_full<64, 4>(a, grid, s);
+  } else if (a.hd <= 128) {
+    rc = nq == 1 ? launch_paged_full<128, 1>(a, grid, s) : nq == 2 ? launch_paged_full<128, 2>(a, grid, s) : launch_paged_full<128, 4>(a, grid, s);
+  } else {
+    rc = nq == 1 ? launch_paged_full<256, 1>(a, grid, s) : launch_paged_full<256, 2>(a, grid, s);
+  }
+  if (rc) return rc;
+  if (a.n_splits > 1) {
+    const int64_t waves = (int64_t)a.b.total_rows * a.H;
+    const unsigned blocks = (unsigned)((waves + 3) / 4);
+    if (dtype == PT_F32) hipLaunchKernelGGL(paged_combine_kernel<float>, dim3(blocks), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(paged_combine_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, a);
+  }
+  PT_HIP_CHECK(hipGetLastError());
+  return PT_OK;
+}

@@ -1,0 +1,74 @@
+// Internal declarations of the serving operators (paged cache, page copies, sampling): kernel arguments and launchers.
+#ifndef PT_SERVING_H_
+#define PT_SERVING_H_
+
+#include "pt_internal.h"
+
+// Bits of pt_paged_batch.status.
+enum { PT_PAGED_BAD_PAGE = 1, PT_PAGED_BAD_LENGTH = 2 };
+
+// The batch as the kernels see it: pt_paged_batch with its bounds resolved.
+struct pt_paged_rows {
+  const int32_t* row_start;
+  const int32_t* kv_len;
+  const int32_t* pages;
+  int64_t pages_stride;
+  int32_t* status;
+  int32_t n_seqs, total_rows, max_q_len, max_kv_len, n_pages, page_shift;
+};
+
+struct pt_append_args {
+  pt_paged_rows b;
+  const void* q;
+  void* q_out;
+  const void* k;
+  const void* v;
+  int64_t q_rs, q_hs, qo_rs, qo_hs, k_rs, k_hs, v_rs, v_hs;   // row and head strides, elements
+  void* kc;                                                  // the layer's pages
+  void* vc;
+  int64_t page_stride, head_stride, token_stride;
+  int32_t H, Hkv, hd;
+};
+
+struct pt_paged_attn_args {
+  pt_paged_rows b;
+  const void* q;
+  void* o;
+  const void* kc;
+  const void* vc;
+  int64_t q_rs, q_hs, o_rs, o_hs;
+  int64_t page_stride, head_stride, token_stride;
+  float* part_o;     // [n_splits][total_rows][H][hd] unscaled sums
+  float2* part_ml;   // [n_splits][total_rows][H] (reference of the exponents in binary orders, sum)
+  float scale_log2;  // |scale| * log2 e, or 1 where the scale is 0
+  float q_sign;      // what the queries are multiplied with for that: 1, -1 or 0
+  int32_t causal, H, Hkv, hd;
+  int32_t tile_rows, tiles, chunk, n_splits;
+};
+
+// How a batch is cut: rows (row, head of the group) per tile, upper bound of the number of tiles, keys per range.
+struct pt_paged_plan {
+  int32_t tile_rows, tiles, chunk, n_splits;
+  size_t off_ml, bytes;   // workspace: part_o first
+};
+
+int pt_launch_paged_append(const pt_append_args& a, const pt_rope* rope, int32_t dtype, hipStream_t s);
+int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const pt_paged_rows& b, pt_paged_plan* p);
+int pt_launch_paged_attn(const pt_paged_attn_args& a, int32_t dtype, hipStream_t s);
+int pt_launch_page_copy(const pt_paged_cache& c, const int32_t* pairs, int32_t n, hipStream_t s);
+size_t pt_sample_workspace(int32_t rows, int32_t vocab);
+struct pt_sample_args {
+  const float* logits;
+  int64_t row_stride;
+  const float* uniform;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* out;
+  void* ws;
+  int32_t rows, vocab;
+};
+int pt_launch_sample(const pt_sample_args& a, hipStream_t s);
+
+#endif  // PT_SERVING_H_
