@@ -201,51 +201,51 @@ def pt_argmax(logits, out=None, stream=None):
 
 
 # -- serving over a paged cache ------------------------------------------------------------------
+# A decode step makes these calls once per layer, and the GPU is done with a small one in a few microseconds: descriptors
+# are built once, tensors are looked at once per call.
 
 def _need(ok: bool, what: str) -> None:
     if not ok:
         raise PTError(PT_ERR_INVALID_ARGUMENT, what)
 
 
-class _on:
-    """Runs a call on a tensor's device and on `stream` (None: that device's current stream)."""
-
-    def __init__(self, tensor, stream=None):
-        import torch
-        self.device, self.stream = tensor.device, stream
-        _need(self.device.type == "cuda", "the tensors must be on a GPU")
-        self.guard = None if torch.cuda.current_device() == self.device.index else torch.cuda.device(self.device)
-
-    def __enter__(self):
-        import torch
-        if self.guard is not None:
-            self.guard.__enter__()
-        st = torch.cuda.current_stream(self.device) if self.stream is None else self.stream
-        return getattr(st, "cuda_stream", st)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-        return False
+def _launch(index: int, stream, fn, *args) -> None:
+    """fn(*args, stream) on GPU `index`, on its current stream if none is given."""
+    import torch
+    if index < 0:
+        raise PTError(PT_ERR_INVALID_ARGUMENT, "the tensors must be on a GPU")
+    st = torch._C._cuda_getCurrentRawStream(index) if stream is None else getattr(stream, "cuda_stream", stream)
+    if torch._C._cuda_getDevice() == index:
+        rc = fn(*args, st)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, st)
+    if rc:
+        _check(rc)
 
 
 def _empty(shape, dtype, device, stream):
     """A tensor for a call on `stream`, allocated on that stream, so that neither earlier nor later owners of its memory
     overlap the call."""
     import torch
+    _need(device.type == "cuda", "the tensors must be on a GPU")
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream, device=device)):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _scratch(given, nbytes: int, device, stream):
-    """(workspace, its bytes): the caller's, or one for this call."""
-    import torch
+def _scratch(given, nbytes, device, stream):
+    """(workspace, its address, its bytes): the caller's, or one of nbytes() for this call."""
     if given is None:
-        return (None, 0) if nbytes == 0 else (_empty(nbytes, torch.uint8, device, stream), nbytes)
+        import torch
+        n = nbytes()
+        if n == 0:
+            return None, None, 0
+        given = _empty(n, torch.uint8, device, stream)
+        return given, given.data_ptr(), n
     _need(given.device == device and given.is_contiguous(), "workspace must be contiguous and on the operands' device")
-    return given, given.numel() * given.element_size()
+    return given, given.data_ptr(), given.numel() * given.element_size()
 
 
 class PTRope:
@@ -275,7 +275,8 @@ class PTPagedCache:
               "k and v must have the same strides and a contiguous last dimension")
         if k.shape[3] == 1:
             st[3] = k.shape[4]
-        self.k, self.v = k, v
+        self.k, self.v, self.dtype, self.index = k, v, k.dtype, k.get_device()
+        self.kv_heads, self.page_size, self.width = k.shape[2:]
         self.c = pt_paged_cache(k.data_ptr(), v.data_ptr(), PT_F32 if k.dtype == torch.float32 else PT_BF16, k.shape[0], k.shape[1],
                                 k.shape[3], k.shape[2], k.shape[4], st[0], st[1], st[2], st[3])
 
@@ -299,46 +300,50 @@ class PTPagedBatch:
         self.width = pages.shape[1]
         _need(n <= 1 or pages.stride(0) >= self.width, "the rows of pages overlap")
         self.row_start, self.kv_len, self.pages, self.status = row_start, kv_len, pages, status
+        self.total_rows, self.index = total_rows, pages.get_device()
         self.c = pt_paged_batch(row_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), self.width if n <= 1 else pages.stride(0), n,
                                 total_rows, max_q_len, max_kv_len, _ptr(status))
         self.given = max_kv_len
 
     def bound(self, cache):
         """The C descriptor with max_kv_len filled in from the table's width where it was not given."""
-        room = self.width * cache.c.page_size
-        _need(self.given <= room, "max_kv_len exceeds the page table")
-        self.c.max_kv_len = self.given or min(room, 0x7fffffff)
+        _need(self.index == cache.index, "batch and cache must be on one device")
+        room = self.width * cache.page_size
+        if self.given == 0:
+            self.c.max_kv_len = min(room, 0x7fffffff)
+        else:
+            _need(self.given <= room, "max_kv_len exceeds the page table")
         return self.c
 
 
 def _rows(t, name: str, cache, batch, heads: int = 0):
-    """pt_head_rows of a device tensor [rows, heads, head width]."""
-    _need(t.dim() == 3 and t.dtype == cache.k.dtype and t.device == cache.k.device, "%s must be [rows, heads, width] of the cache's type and device" % name)
-    _need(t.shape[0] >= batch.c.total_rows and t.shape[2] == cache.c.head_dim, "%s is too small or of another head width" % name)
-    _need(heads == 0 or t.shape[1] == heads, "%s has %d heads, not %d" % (name, t.shape[1], heads))
-    _need(t.stride(2) == 1, "the last dimension of %s must be contiguous" % name)
-    st = t.stride()
-    return pt_head_rows(t.data_ptr(), 0 if t.shape[0] == 1 else st[0], 0 if t.shape[1] == 1 else st[1])
+    """(pt_head_rows, heads) of a device tensor [rows, heads, head width]."""
+    shape, st = t.shape, t.stride()
+    if not (len(shape) == 3 and t.dtype is cache.dtype and t.get_device() == cache.index):
+        raise PTError(PT_ERR_INVALID_ARGUMENT, "%s must be [rows, heads, width] of the cache's type and device" % name)
+    n, h, w = shape
+    if not (n >= batch.total_rows and w == cache.width and (heads == 0 or h == heads) and st[2] == 1):
+        raise PTError(PT_ERR_INVALID_ARGUMENT, "%s has shape %s and strides %s: need %d rows of %s heads of %d contiguous elements"
+                      % (name, tuple(shape), st, batch.total_rows, heads or "any", cache.width))
+    # the stride of a dimension of one entry says nothing
+    return pt_head_rows(t.data_ptr(), st[0] if n > 1 else 0, st[1] if h > 1 else 0), h
 
 
 def pt_paged_append(cache: PTPagedCache, layer: int, batch: PTPagedBatch, k, v, q=None, q_out=None, rope: Optional[PTRope] = None, stream=None):
     """Stores the batch's keys and values [rows, kv heads, width] in their pages, queries and keys rotated on the way.
     q [rows, heads, width] goes to q_out (made if not given; may be q).  Returns q_out."""
-    kv = cache.c.n_kv_heads
     cb = batch.bound(cache)
-    _need(batch.pages.device == cache.k.device, "batch and cache must be on one device")
-    ck, cv = _rows(k, "k", cache, batch, kv), _rows(v, "v", cache, batch, kv)
-    with _on(cache.k, stream) as st:
-        cq = co = None
-        heads = 0
-        if q is not None:
-            heads = q.shape[1]
-            if q_out is None:
-                q_out = _empty(q.shape, q.dtype, q.device, stream)
-            cq, co = _rows(q, "q", cache, batch), _rows(q_out, "q_out", cache, batch, heads)
-        else:
-            _need(q_out is None, "q_out without q")
-        _check(lib().pt_paged_append(cache.c, layer, cb, None if rope is None else rope.c, cq, co, heads, ck, cv, st))
+    ck, cv = _rows(k, "k", cache, batch, cache.kv_heads)[0], _rows(v, "v", cache, batch, cache.kv_heads)[0]
+    cq = co = None
+    heads = 0
+    if q is not None:
+        cq, heads = _rows(q, "q", cache, batch)
+        if q_out is None:
+            q_out = _empty(q.shape, q.dtype, q.device, stream)
+        co = _rows(q_out, "q_out", cache, batch, heads)[0]
+    else:
+        _need(q_out is None, "q_out without q")
+    _launch(cache.index, stream, lib().pt_paged_append, cache.c, layer, cb, None if rope is None else rope.c, cq, co, heads, ck, cv)
     return q_out
 
 
@@ -354,16 +359,13 @@ def pt_paged_attention(cache: PTPagedCache, layer: int, batch: PTPagedBatch, q, 
     """Attention of the batch's queries [rows, heads, width] over their sequences' pages.  scale: 1 / sqrt(width) if not
     given.  workspace: uint8 device tensor of pt_paged_attention_bytes (made per call if not given).  Returns out."""
     cb = batch.bound(cache)
-    _need(batch.pages.device == cache.k.device, "batch and cache must be on one device")
-    cq = _rows(q, "q", cache, batch)
-    heads = q.shape[1]
-    with _on(cache.k, stream) as st:
-        if out is None:
-            out = _empty(q.shape, q.dtype, q.device, stream)
-        co = _rows(out, "out", cache, batch, heads)
-        ws, size = _scratch(workspace, 0 if workspace is not None else pt_paged_attention_bytes(cache, batch, heads), q.device, stream)
-        _check(lib().pt_paged_attention(cache.c, layer, cb, cq, co, heads, q.shape[2] ** -0.5 if scale is None else scale, int(causal),
-                                        _ptr(ws), size, st))
+    cq, heads = _rows(q, "q", cache, batch)
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    co = _rows(out, "out", cache, batch, heads)[0]
+    ws, at, size = _scratch(workspace, lambda: pt_paged_attention_bytes(cache, batch, heads), q.device, stream)
+    _launch(cache.index, stream, lib().pt_paged_attention, cache.c, layer, cb, cq, co, heads, cache.width ** -0.5 if scale is None else scale,
+            int(causal), at, size)
     return out
 
 
@@ -376,8 +378,7 @@ def pt_page_copy(cache: PTPagedCache, pairs, stream=None) -> None:
     if p.dtype != np.int32:
         _need(int(p.min()) >= 0 and int(p.max()) < 2 ** 31, "a page out of range")
     p = np.ascontiguousarray(p, dtype=np.int32)
-    with _on(cache.k, stream) as st:
-        _check(lib().pt_page_copy(cache.c, p.ctypes.data, p.shape[0], st))
+    _launch(cache.index, stream, lib().pt_page_copy, cache.c, p.ctypes.data, p.shape[0])
 
 
 def pt_sample_bytes(rows: int, vocab: int) -> int:
@@ -387,23 +388,31 @@ def pt_sample_bytes(rows: int, vocab: int) -> int:
     return n.value
 
 
+def _row_params(t, dtype, rows: int, index: int, name: str):
+    """Address of a parameter with one entry per row, or None."""
+    if t is None:
+        return None
+    if not (t.dtype is dtype and t.shape == (rows,) and t.get_device() == index and (rows <= 1 or t.stride(0) == 1)):
+        raise PTError(PT_ERR_INVALID_ARGUMENT, "%s must be contiguous %s [rows] on the logits' device" % (name, str(dtype)[6:]))
+    return t.data_ptr()
+
+
 def pt_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, out=None, workspace=None, stream=None):
     """One token per row of logits (float32 device tensor [rows, vocab], rows contiguous) by the given uniform numbers [rows]
     in [0, 1).  temperature, top_p, min_p: float32 [rows], top_k: int32 [rows], or None.  Returns int32 [rows]."""
     import torch
-    _need(logits.dim() == 2 and logits.dtype == torch.float32 and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits must be float32 [rows, vocab] with contiguous rows")
-    rows, vocab = logits.shape
-    for t, ty, name in ((uniform, torch.float32, "uniform"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
-                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (out, torch.int32, "out")):
-        if t is not None or name == "uniform":
-            _need(t is not None and t.dtype == ty and t.shape == (rows,) and t.device == logits.device and (rows <= 1 or t.stride(0) == 1),
-                  "%s must be contiguous %s [rows] on the logits' device" % (name, str(ty)[6:]))
-    with _on(logits, stream) as st:
-        if out is None:
-            out = _empty((rows,), torch.int32, logits.device, stream)
-        ws, size = _scratch(workspace, 0 if workspace is not None else pt_sample_bytes(rows, vocab), logits.device, stream)
-        _check(lib().pt_sample(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab, uniform.data_ptr(), _ptr(temperature), _ptr(top_k),
-                               _ptr(top_p), _ptr(min_p), out.data_ptr(), _ptr(ws), size, st))
+    f32, i32 = torch.float32, torch.int32
+    _need(logits.dim() == 2 and logits.dtype is f32, "logits must be float32 [rows, vocab]")
+    (rows, vocab), st, index = logits.shape, logits.stride(), logits.get_device()
+    _need(st[1] == 1 or vocab == 1, "the rows of logits must be contiguous")
+    _need(uniform is not None, "uniform is missing")
+    params = (_row_params(uniform, f32, rows, index, "uniform"), _row_params(temperature, f32, rows, index, "temperature"),
+              _row_params(top_k, i32, rows, index, "top_k"), _row_params(top_p, f32, rows, index, "top_p"), _row_params(min_p, f32, rows, index, "min_p"))
+    if out is None:
+        out = _empty((rows,), i32, logits.device, stream)
+    to = _row_params(out, i32, rows, index, "out")
+    ws, at, size = _scratch(workspace, lambda: pt_sample_bytes(rows, vocab), logits.device, stream)
+    _launch(index, stream, lib().pt_sample, logits.data_ptr(), st[0] if rows > 1 else vocab, rows, vocab, *params, to, at, size)
     return out
 
 

@@ -29,11 +29,20 @@ __device__ __forceinline__ int paged_vis(const pt_paged_attn_args& a, const page
   return pos < 0 ? 0 : a.causal ? pos + 1 : sq.kv;
 }
 
-// Tile `tile` of the batch; false where there are fewer.  Sequences are scanned 64 at a time (wavefront-uniform result).
+// Rows of a sequence, and whether class WIDE takes it.
+template <bool WIDE>
+__device__ __forceinline__ bool paged_in_class(const pt_paged_attn_args& a, int n) {
+  return n > 0 && (n * (int64_t)(a.H / a.Hkv) > a.few) == WIDE;
+}
+
+// Tile `tile` of the class's sequences; false where there are fewer.  Where no sequence has more than one tile, tile and
+// sequence are one; otherwise sequences are scanned 64 at a time (wavefront-uniform result).
+template <bool WIDE>
 __device__ __forceinline__ bool paged_find_tile(const pt_paged_attn_args& a, int tile, paged_tile* t) {
   const int G = a.H / a.Hkv, lane = threadIdx.x & 63;
+  const pt_paged_cut& cut = a.cut[WIDE];
   int seq = tile, in_seq = 0;
-  if (a.b.max_q_len * (int64_t)G > a.tile_rows) {   // more than one tile per sequence is possible
+  if (WIDE || min(a.b.max_q_len * (int64_t)G, (int64_t)a.few) > cut.tile_rows) {
     int before = 0;
     seq = -1;
     for (int base = 0; base < a.b.n_seqs; base += 64) {
@@ -42,7 +51,7 @@ __device__ __forceinline__ bool paged_find_tile(const pt_paged_attn_args& a, int
         const int r0 = a.b.row_start[base + lane], r1 = a.b.row_start[base + lane + 1];
         const int first = min(max(r0, 0), a.b.total_rows);
         const int rows = min(min(max(r1, first), a.b.total_rows) - first, a.b.max_q_len);
-        n = (int)(((int64_t)rows * G + a.tile_rows - 1) / a.tile_rows);
+        if (paged_in_class<WIDE>(a, rows)) n = (int)(((int64_t)rows * G + cut.tile_rows - 1) / cut.tile_rows);
       }
       int sum = n;   // inclusive over the lanes
 #pragma unroll
@@ -65,12 +74,13 @@ __device__ __forceinline__ bool paged_find_tile(const pt_paged_attn_args& a, int
   in_seq = __builtin_amdgcn_readfirstlane(in_seq);
   t->seq = seq;
   t->sq = paged_load_seq(a.b, seq);
-  t->row0 = in_seq * a.tile_rows;
-  t->nrows = (int)min((int64_t)a.tile_rows, (int64_t)t->sq.n * G - t->row0);
+  if (!paged_in_class<WIDE>(a, t->sq.n)) return false;
+  t->row0 = in_seq * cut.tile_rows;
+  t->nrows = (int)min((int64_t)cut.tile_rows, (int64_t)t->sq.n * G - t->row0);
   if (t->nrows <= 0) return false;
   t->base_pos = t->sq.kv - t->sq.n;
   t->vis = paged_vis(a, t->sq, (t->row0 + t->nrows - 1) / G);
-  t->nsplit = max(1, (int)(((int64_t)t->vis + a.chunk - 1) / a.chunk));
+  t->nsplit = max(1, (int)(((int64_t)t->vis + cut.chunk - 1) / cut.chunk));
   return true;
 }
 
@@ -140,10 +150,10 @@ __device__ __forceinline__ void paged_merge(const pt_paged_attn_args& a, const p
     const int lim = paged_vis(a, t.sq, i);
     float m = -INFINITY, l = 0.f, f[4], o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, red_ml[w * a.tile_rows + r].x);
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, red_ml[w * a.cut[0].tile_rows + r].x);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float2 ml = red_ml[w * a.tile_rows + r];
+      const float2 ml = red_ml[w * a.cut[0].tile_rows + r];
       f[w] = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
       l += f[w] * ml.y;
     }
@@ -151,7 +161,7 @@ __device__ __forceinline__ void paged_merge(const pt_paged_attn_args& a, const p
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) o[j] += f[w] * red_o[(w * a.tile_rows + r) * (HD + 4) + lane + 64 * j];
+      for (int w = 0; w < 4; ++w) o[j] += f[w] * red_o[(w * a.cut[0].tile_rows + r) * (HD + 4) + lane + 64 * j];
       if (lane + 64 * j < a.hd) odd |= !(fabsf(o[j]) < INFINITY);
     }
     if (__any(odd)) {
@@ -195,10 +205,10 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
   const int l16 = lane & 15, g = lane >> 4;
   const int kvh = blockIdx.x % a.Hkv;
   const int rest = blockIdx.x / a.Hkv;
-  const int split = rest / a.tiles;
+  const int split = rest / a.cut[0].tiles;
   paged_tile t;
-  if (!paged_find_tile(a, rest - split * a.tiles, &t) || split >= t.nsplit) return;
-  const int k0 = split * a.chunk, k1 = min(t.vis, k0 + a.chunk);
+  if (!paged_find_tile<false>(a, rest - split * a.cut[0].tiles, &t) || split >= t.nsplit) return;
+  const int k0 = split * a.cut[0].chunk, k1 = min(t.vis, k0 + a.cut[0].chunk);
   const int G = a.H / a.Hkv;
 
   // queries: B operand of S^T, and each one's first key that it does not see
@@ -392,6 +402,263 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
 }
 
 // ------------------------------------------------------------------------------------------------
+// bf16, many rows: four wavefronts of 32 packed rows each share key tiles of 64 (K and V as they lie in their pages, two
+// tiles in LDS: one that is read, one on its way).  A wavefront loads the tile's 16 keys of its number - one page - and
+// multiplies all 64 with its own rows; MFMA layouts, swizzle and transposing reads as above.
+// The loads to LDS are inline assembly: the compiler takes any LDS read to depend on such a load of its own and waits for
+// all of them in front of it, that is for the next tile in front of this one's first product.  They have no result
+// registers; what waits for them is written out below, one wait and one barrier per tile.
+// ------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+
+template <int HD, bool FULL>
+__global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_attn_args a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  using geo = paged_geom<HD>;
+  constexpr int TK = 64, CH = geo::CH, RPI = geo::RPI, PER16 = geo::PER16, TILE_B = geo::TILE_B, ROWB = geo::ROWB;
+  constexpr int NB = TK / 16, KS = HD / 32, HB = HD / 16, NU = TK / 32, NQ = 2;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [2][K tile, V tile]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % a.Hkv;
+  const int rest = blockIdx.x / a.Hkv;
+  const int split = rest / a.cut[1].tiles;
+  paged_tile t;
+  // the last tiles of a sequence see most: they come first
+  if (!paged_find_tile<true>(a, a.cut[1].tiles - 1 - (rest - split * a.cut[1].tiles), &t) || split >= t.nsplit) return;
+  const int k0 = split * a.cut[1].chunk, k1 = min(t.vis, k0 + a.cut[1].chunk);
+  const int G = a.H / a.Hkv;
+  const int w0 = wave * NQ * 16;   // the wavefront's first row in the tile
+
+  bf16x8_t qf[NQ][KS];
+  int lim[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = t.row0 + w0 + n * 16 + l16, i = r / G, hh = r - i * G;
+    const bool real = w0 + n * 16 + l16 < t.nrows;
+    lim[n] = real ? min(paged_vis(a, t.sq, i), k1) : 0;
+    const bf16_t* q = (const bf16_t*)a.q + (t.sq.first + i) * a.q_rs + (kvh * G + hh) * a.q_hs;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (real && (FULL || kk * 32 + g * 8 < a.hd)) w = *(const uint4*)(q + kk * 32 + g * 8);
+      if (a.q_sign != 1.0f) {
+        const uint32_t keep = a.q_sign == 0.0f ? 0u : 0xffffffffu, flip = a.q_sign < 0.0f ? 0x80008000u : 0u;
+        w.x = (w.x & keep) ^ flip; w.y = (w.y & keep) ^ flip; w.z = (w.z & keep) ^ flip; w.w = (w.w & keep) ^ flip;
+      }
+      qf[n][kk] = *(const bf16x8_t*)&w;
+    }
+  }
+  // the keys that this wavefront's first and last rows see (no row: none)
+  const int w_rows = min(NQ * 16, t.nrows - w0);
+  const int lim_first = w_rows > 0 ? min(paged_vis(a, t.sq, (t.row0 + w0) / G), k1) : 0;
+  const int lim_last = w_rows > 0 ? min(paged_vis(a, t.sq, (t.row0 + w0 + w_rows - 1) / G), k1) : 0;
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)smem;
+  if (!FULL)
+    for (int i = tid; i < 4 * TILE_B / 16; i += 256) ((uint4*)smem)[i] = make_uint4(0, 0, 0, 0);
+  uint32_t voff[PER16];
+  bool on[PER16];
+#pragma unroll
+  for (int i = 0; i < PER16; ++i) {
+    const int row = i * RPI + lane / CH, c = (lane % CH) ^ geo::swz(row);
+    voff[i] = (uint32_t)(row * a.token_stride * 2 + c * 16);
+    on[i] = FULL || c * 8 < a.hd;
+  }
+  typedef const __attribute__((address_space(4))) int32_t* cptr_t;
+  const cptr_t pages = (cptr_t)(a.b.pages + t.seq * a.b.pages_stride);
+  const int mask = (1 << a.b.page_shift) - 1;
+  // page of the wavefront's 16 keys of the tile (of the range's last key where those are behind it)
+  auto page_id = [&](int kb) { return pages[min(kb + 16 * wave, k1 - 1) >> a.b.page_shift]; };
+  auto load_tile = [&](int kb, int page, uint32_t stage) {
+    if ((unsigned)page >= (unsigned)a.b.n_pages) {
+      paged_raise(a.b, PT_PAGED_BAD_PAGE);
+      page = 0;
+    }
+    const int64_t at = (page * a.page_stride + ((kb + 16 * wave) & mask) * a.token_stride + kvh * a.head_stride) * 2;
+    const char* k = (const char*)a.kc + at;
+    const char* v = (const char*)a.vc + at;
+    const uint32_t lds = lds0 + stage + wave * 16 * ROWB;
+#pragma unroll
+    for (int i = 0; i < PER16; ++i)
+      if (on[i]) load_to_lds(lds + i * 1024, k, voff[i]);
+#pragma unroll
+    for (int i = 0; i < PER16; ++i)
+      if (on[i]) load_to_lds(lds + TILE_B + i * 1024, v, voff[i]);
+  };
+
+  // LDS addresses of the fragments of the first 16 keys
+  uint32_t ka[KS], va[HB];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) ka[kk] = lds0 + l16 * ROWB + (((kk * 4 + g) ^ geo::swz(l16)) * 16);
+  const int vrow = 4 * g + (l16 >> 2);
+#pragma unroll
+  for (int hb = 0; hb < HB; ++hb) va[hb] = lds0 + TILE_B + vrow * ROWB + (((hb * 2 + ((l16 & 3) >> 1)) ^ geo::swz(vrow)) * 16) + (l16 & 1) * 8;
+  typedef const __attribute__((address_space(3))) bf16x8_t* lk_t;
+
+  f32x4_t acc[NQ][HB];
+  float m_run[NQ], l_run[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    m_run[n] = -INFINITY;
+    l_run[n] = 0.f;
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) acc[n][hb] = {0.f, 0.f, 0.f, 0.f};
+  }
+  const float c_log2 = a.scale_log2;
+  if (!FULL) __syncthreads();   // the zeros are in LDS
+  uint32_t stage = 0;
+  int next_page = 0;
+  if (k0 < k1) {
+    load_tile(k0, page_id(k0), 0);
+    next_page = page_id(min(k0 + TK, k1 - 1));
+  }
+  for (int kb = k0; kb < k1; kb += TK) {
+    // this tile's loads are done, here and in the other wavefronts; nobody reads the other stage any more
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (kb + TK < k1) {
+      load_tile(kb + TK, next_page, stage ^ (2 * TILE_B));
+      next_page = page_id(min(kb + 2 * TK, k1 - 1));
+    } else if (kb + TK > k1) {
+      // positions behind the range are not data: their values become 0, so that 0 * x stays 0
+      for (int i = (k1 - kb) * CH + tid; i < TK * CH; i += 256) ((uint4*)(smem + stage + TILE_B))[i] = make_uint4(0, 0, 0, 0);
+      __syncthreads();
+    }
+    if (kb < lim_last) {   // wavefront-uniform: some row sees some key of the tile
+      f32x4_t s[NQ][NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+          const bf16x8_t kf = *(lk_t)(uintptr_t)(ka[kk] + stage + b * 16 * ROWB);
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) {
+            if (kk == 0) s[n][b] = {0.f, 0.f, 0.f, 0.f};
+            s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][kk], s[n][b], 0, 0, 0);
+          }
+        }
+      }
+      union {
+        uint32_t u[4];
+        bf16x8_t v;
+      } pf[NQ][NU];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        if (kb + TK > lim_first) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+              if (kb + 16 * b + 4 * g + v >= lim[n]) s[n][b][v] = -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[n][b][v]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        // The reference of the exponentials moves only when the maximum exceeds it by more than 8 binary orders; until
+        // then the probabilities stay below 2^8, which fp32 sums and bf16 operands hold as well, and nothing is rescaled.
+        const bool grow = (mx - m_run[n]) * c_log2 > 8.0f;
+        if (__any(grow)) {
+          const float m_new = grow ? mx : m_run[n];
+          const float corr = grow ? __builtin_amdgcn_exp2f((m_run[n] - m_new) * c_log2) : 1.0f;
+          m_run[n] = m_new;
+          l_run[n] *= corr;
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb) acc[n][hb] *= corr;
+        }
+        const float mc = m_run[n] == -INFINITY ? 0.f : m_run[n] * c_log2;
+        float psum = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            s[n][b][v] = __builtin_amdgcn_exp2f(fmaf(s[n][b][v], c_log2, -mc));
+            psum += s[n][b][v];
+          }
+        l_run[n] += psum;
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) pf[n][u].u[j] = pack_bf16x2(s[n][2 * u + (j >> 1)][2 * (j & 1)], s[n][2 * u + (j >> 1)][2 * (j & 1) + 1]);
+      }
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          union {
+            s16x4_t h[2];
+            bf16x8_t v;
+          } vf;
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr4_t)(uintptr_t)(va[hb] + stage + (32 * u + 16 * x) * ROWB));
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) acc[n][hb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[n][u].v, acc[n][hb], 0, 0, 0);
+        }
+    }
+    stage ^= 2 * TILE_B;
+  }
+  // acc[n][hb], register v: element 16 hb + 4 g + v of query n * 16 + l16
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    float l = l_run[n] + __shfl_xor(l_run[n], 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    const float m = m_run[n] * c_log2;
+    const int r = t.row0 + w0 + n * 16 + l16, i = r / G, head = kvh * G + (r - i * G), row = t.sq.first + i;
+    const bool real = w0 + n * 16 + l16 < t.nrows;
+    const int see = paged_vis(a, t.sq, i);
+    bool odd = !(fabsf(l) < INFINITY);
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) odd |= !(fabsf(acc[n][hb][v]) < INFINITY);
+    odd &= real;
+    if (real) {
+      const int64_t at = ((int64_t)split * a.b.total_rows + row) * a.H + head;
+      if (t.nsplit == 1) {
+        const float inv = see <= 0 ? 0.f : 1.0f / l;
+        bf16_t* o = (bf16_t*)a.o + row * a.o_rs + head * a.o_hs + 4 * g;
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb)
+          if (FULL || hb * 16 + 4 * g < a.hd) {
+            uint2 w;
+            w.x = pack_bf16x2(acc[n][hb][0] * inv, acc[n][hb][1] * inv);
+            w.y = pack_bf16x2(acc[n][hb][2] * inv, acc[n][hb][3] * inv);
+            *(uint2*)(o + hb * 16) = w;
+          }
+      } else {
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb)
+          if (FULL || hb * 16 + 4 * g < a.hd) *(f32x4_t*)(a.part_o + at * a.hd + hb * 16 + 4 * g) = acc[n][hb];
+        if (g == 0) a.part_ml[at] = make_float2(m, l);
+      }
+    }
+    // rows that met an infinity or a NaN: again, without the keys behind them
+    uint64_t again = __ballot(odd);
+    again |= again >> 32;
+    again |= again >> 16;
+    for (int j = 0; j < 16; ++j)
+      if (again >> j & 1) {
+        const int rj = t.row0 + w0 + n * 16 + j, ij = rj / G, hj = kvh * G + (rj - ij * G), rowj = t.sq.first + ij;
+        const int limj = paged_vis(a, t.sq, ij);
+        const int64_t hoff = (int64_t)kvh * a.head_stride;
+        float mj, lj, oj[4];
+        paged_row_alone<bf16_t>(a, (const bf16_t*)a.q + rowj * a.q_rs + hj * a.q_hs, (const bf16_t*)a.kc + hoff, (const bf16_t*)a.vc + hoff,
+                                a.b.pages + t.seq * a.b.pages_stride, k0, min(k1, limj), &mj, &lj, oj);
+#pragma unroll
+        for (int e = 0; e < HD / 64; ++e)
+          if (lane + 64 * e < a.hd) paged_store_row<bf16_t>(a, t, split, rowj, hj, limj, mj, lj, oj[e], lane + 64 * e);
+      }
+  }
+#endif
+}
+
+// ------------------------------------------------------------------------------------------------
 // fp32, on 16x16x4 MFMAs: 16 packed rows per workgroup, 16 keys per wavefront and step, operands straight from the pages.
 // The contraction over the head takes elements 16 j + 4 g + i in step (j, i), so that a lane's operands are 16-byte loads; the
 // second product's rows are head elements 64 hb + 4 r + j for the same reason.
@@ -404,10 +671,10 @@ __global__ void __launch_bounds__(256, 1) paged_attn_f32_kernel(const pt_paged_a
   const int l16 = lane & 15, g = lane >> 4;
   const int kvh = blockIdx.x % a.Hkv;
   const int rest = blockIdx.x / a.Hkv;
-  const int split = rest / a.tiles;
+  const int split = rest / a.cut[0].tiles;
   paged_tile t;
-  if (!paged_find_tile(a, rest - split * a.tiles, &t) || split >= t.nsplit) return;
-  const int k0 = split * a.chunk, k1 = min(t.vis, k0 + a.chunk);
+  if (!paged_find_tile<false>(a, rest - split * a.cut[0].tiles, &t) || split >= t.nsplit) return;
+  const int k0 = split * a.cut[0].chunk, k1 = min(t.vis, k0 + a.cut[0].chunk);
   const int G = a.H / a.Hkv;
   f32x4_t qf[KJ];
   const int r = t.row0 + l16, qi = r / G, hh = r - qi * G;
@@ -523,9 +790,10 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const pt_paged_attn_
   if (row < sq.first || row >= sq.first + sq.n) return;
   const int G = a.H / a.Hkv;
   const int i = row - sq.first;
-  const int tile = (i * G + head % G) / a.tile_rows;
-  const int64_t last = min((int64_t)(tile + 1) * a.tile_rows, (int64_t)sq.n * G) - 1;
-  const int nsplit = (int)(((int64_t)paged_vis(a, sq, (int)(last / G)) + a.chunk - 1) / a.chunk);
+  const pt_paged_cut& cut = a.cut[paged_in_class<true>(a, sq.n)];
+  const int tile = (i * G + head % G) / cut.tile_rows;
+  const int64_t last = min((int64_t)(tile + 1) * cut.tile_rows, (int64_t)sq.n * G) - 1;
+  const int nsplit = (int)(((int64_t)paged_vis(a, sq, (int)(last / G)) + cut.chunk - 1) / cut.chunk);
   if (nsplit <= 1) return;
   const int64_t step = (int64_t)a.b.total_rows * a.H, at = (int64_t)row * a.H + head;
   float2 ml = make_float2(-INFINITY, 0.f);
@@ -541,28 +809,42 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const pt_paged_attn_
   }
 }
 
-static int paged_blocks(int32_t dtype, int32_t hd, int64_t rows_max) {   // blocks of 16 packed rows per tile
-  if (dtype == PT_F32 || rows_max <= 16) return 1;
-  return rows_max <= 32 || hd > 128 ? 2 : 4;
+constexpr int PA_WIDE_ROWS = 128;
+
+// Ranges of keys for `units` workgroups: as many as it takes to have `want` of them, each of at least `least` keys.
+static void paged_ranges(int64_t units, int64_t keys, int64_t want, int64_t least, pt_paged_cut* c) {
+  int64_t splits = std::min<int64_t>((want + units - 1) / units, PA_MAX_SPLITS);
+  const int64_t chunk = ((keys + splits - 1) / splits + least - 1) / least * least;
+  c->chunk = (int32_t)chunk;
+  c->n_splits = (int32_t)((keys + chunk - 1) / chunk);
 }
 
 int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const pt_paged_rows& b, pt_paged_plan* p) {
-  const int64_t G = H / Hkv, rows_max = b.max_q_len * G;
+  const int64_t G = H / Hkv, rows_max = b.max_q_len * G, keys = std::max(b.max_kv_len, 1);
   if (rows_max > 0x3fffffff) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "max_q_len times the heads of a group is too large");
-  p->tile_rows = 16 * paged_blocks(dtype, hd, rows_max);
-  int64_t tiles = b.n_seqs;
-  if (rows_max > p->tile_rows)
-    tiles = std::min(b.n_seqs * ((rows_max + p->tile_rows - 1) / p->tile_rows), b.total_rows * G / p->tile_rows + b.n_seqs);
-  const int64_t units = tiles * Hkv;
+  const bool wide = dtype == PT_BF16 && hd <= 128 && rows_max > 32;
+  // Blocks of 16 packed rows in a tile of the few-row kernels: what the longest sequence needs, or beside longer ones, what a
+  // single new row needs.
+  const int64_t few = wide ? (G <= 32 ? G : 0) : rows_max;
+  const int nq = dtype == PT_F32 || few <= 16 ? 1 : 2;
+  p->cut[0].tile_rows = 16 * nq;
+  p->few = wide ? (few > 0 ? 16 * nq : 0) : 0x7fffffff;
+  int64_t t0 = wide && few == 0 ? 0 : b.n_seqs, t1 = 0;
+  if (!wide && rows_max > 16 * nq)
+    t0 = std::min(b.n_seqs * ((rows_max + 16 * nq - 1) / (16 * nq)), b.total_rows * G / (16 * nq) + b.n_seqs);
+  if (wide) {
+    const int64_t seqs = std::min<int64_t>(b.n_seqs, b.total_rows * G / (p->few + 1));
+    t1 = std::min(seqs * ((rows_max + PA_WIDE_ROWS - 1) / PA_WIDE_ROWS), b.total_rows * G / PA_WIDE_ROWS + seqs);
+    p->cut[1].tile_rows = PA_WIDE_ROWS;
+  }
+  p->cut[0].tiles = (int32_t)std::min<int64_t>(t0, 0x7fffffff);
+  p->cut[1].tiles = (int32_t)std::min<int64_t>(t1, 0x7fffffff);
   // enough ranges for 2048 workgroups, each of at least a tile for every wavefront
-  int64_t splits = std::min<int64_t>((2048 + units - 1) / units, PA_MAX_SPLITS);
-  int64_t chunk = (std::max(b.max_kv_len, 1) + splits - 1) / splits;
-  chunk = (chunk + 255) / 256 * 256;
-  splits = (std::max(b.max_kv_len, 1) + chunk - 1) / chunk;
-  if (units * splits > 0x7fffffff || (int64_t)b.total_rows * H > ((int64_t)1 << 32)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
-  p->tiles = (int32_t)tiles;
-  p->chunk = (int32_t)chunk;
-  p->n_splits = (int32_t)splits;
+  if (t0 > 0) paged_ranges(t0 * Hkv, keys, 2048, 256, &p->cut[0]);
+  if (t1 > 0) paged_ranges(t1 * Hkv, keys, 512, 256, &p->cut[1]);
+  if (t0 * Hkv * p->cut[0].n_splits > 0x7fffffff || t1 * Hkv * p->cut[1].n_splits > 0x7fffffff || (int64_t)b.total_rows * H > ((int64_t)1 << 32))
+    return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
+  const int32_t splits = std::max(p->cut[0].n_splits, p->cut[1].n_splits);
   if (splits > 1) {
     const size_t parts = (size_t)splits * b.total_rows * H;
     p->off_ml = (parts * hd * 4 + 15) / 16 * 16;
@@ -590,21 +872,37 @@ static int launch_paged_f32(const pt_paged_attn_args& a, unsigned grid, hipStrea
   return PT_OK;
 }
 
+template <int HD, bool FULL>
+static int launch_wide(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
+  constexpr int LDS = 4 * paged_geom<HD>::TILE_B;
+  auto kern = paged_attn_wide_kernel<HD, FULL>;
+  PT_SET_MAX_LDS_ONCE(kern, LDS);
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), LDS, s, a);
+  return PT_OK;
+}
+
 int pt_launch_paged_attn(const pt_paged_attn_args& a, int32_t dtype, hipStream_t s) {
-  const unsigned grid = (unsigned)((int64_t)a.tiles * a.Hkv * a.n_splits);
-  const int nq = a.tile_rows / 16;
-  int rc;
-  if (dtype == PT_F32) {
-    rc = a.hd <= 64 ? launch_paged_f32<64>(a, grid, s) : a.hd <= 128 ? launch_paged_f32<128>(a, grid, s) : launch_paged_f32<256>(a, grid, s);
-  } else if (a.hd <= 64) {
-    rc = nq == 1 ? launch_paged_full<64, 1>(a, grid, s) : nq == 2 ? launch_paged_full<64, 2>(a, grid, s) : launch_paged_full<64, 4>(a, grid, s);
-  } else if (a.hd <= 128) {
-    rc = nq == 1 ? launch_paged_full<128, 1>(a, grid, s) : nq == 2 ? launch_paged_full<128, 2>(a, grid, s) : launch_paged_full<128, 4>(a, grid, s);
-  } else {
-    rc = nq == 1 ? launch_paged_full<256, 1>(a, grid, s) : launch_paged_full<256, 2>(a, grid, s);
+  int rc = PT_OK;
+  if (a.cut[1].tiles > 0) {
+    const unsigned grid = (unsigned)((int64_t)a.cut[1].tiles * a.Hkv * a.cut[1].n_splits);
+    if (a.hd <= 64) rc = a.hd == 64 ? launch_wide<64, true>(a, grid, s) : launch_wide<64, false>(a, grid, s);
+    else rc = a.hd == 128 ? launch_wide<128, true>(a, grid, s) : launch_wide<128, false>(a, grid, s);
+  }
+  if (!rc && a.cut[0].tiles > 0) {
+    const unsigned grid = (unsigned)((int64_t)a.cut[0].tiles * a.Hkv * a.cut[0].n_splits);
+    const int nq = a.cut[0].tile_rows / 16;
+    if (dtype == PT_F32) {
+      rc = a.hd <= 64 ? launch_paged_f32<64>(a, grid, s) : a.hd <= 128 ? launch_paged_f32<128>(a, grid, s) : launch_paged_f32<256>(a, grid, s);
+    } else if (a.hd <= 64) {
+      rc = nq == 1 ? launch_paged_full<64, 1>(a, grid, s) : launch_paged_full<64, 2>(a, grid, s);
+    } else if (a.hd <= 128) {
+      rc = nq == 1 ? launch_paged_full<128, 1>(a, grid, s) : launch_paged_full<128, 2>(a, grid, s);
+    } else {
+      rc = nq == 1 ? launch_paged_full<256, 1>(a, grid, s) : launch_paged_full<256, 2>(a, grid, s);
+    }
   }
   if (rc) return rc;
-  if (a.n_splits > 1) {
+  if (std::max(a.cut[0].n_splits, a.cut[1].n_splits) > 1) {
     const int64_t waves = (int64_t)a.b.total_rows * a.H;
     const unsigned blocks = (unsigned)((waves + 3) / 4);
     if (dtype == PT_F32) hipLaunchKernelGGL(paged_combine_kernel<float>, dim3(blocks), dim3(256), 0, s, a);

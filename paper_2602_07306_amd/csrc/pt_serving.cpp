@@ -201,7 +201,7 @@ extern "C" int pt_paged_attention(const pt_paged_cache* cache, int32_t layer, co
   a.q_sign = scale == 0.0f ? 0.0f : scale < 0.0f ? -1.0f : 1.0f;
   a.causal = causal != 0;
   a.H = n_heads; a.Hkv = cache->n_kv_heads; a.hd = cache->head_dim;
-  a.tile_rows = plan.tile_rows; a.tiles = plan.tiles; a.chunk = plan.chunk; a.n_splits = plan.n_splits;
+  a.few = plan.few; a.cut[0] = plan.cut[0]; a.cut[1] = plan.cut[1];
   return pt_launch_paged_attn(a, cache->dtype, (hipStream_t)hip_stream);
 }
 

@@ -30,6 +30,12 @@ struct pt_append_args {
   int32_t H, Hkv, hd;
 };
 
+// How the rows of a batch's sequences are cut: rows (new row, head of the group) per tile, upper bound of the number of
+// tiles, keys per range, upper bound of the number of ranges.
+struct pt_paged_cut {
+  int32_t tile_rows, tiles, chunk, n_splits;
+};
+
 struct pt_paged_attn_args {
   pt_paged_rows b;
   const void* q;
@@ -43,12 +49,15 @@ struct pt_paged_attn_args {
   float scale_log2;  // |scale| * log2 e, or 1 where the scale is 0
   float q_sign;      // what the queries are multiplied with for that: 1, -1 or 0
   int32_t causal, H, Hkv, hd;
-  int32_t tile_rows, tiles, chunk, n_splits;
+  // sequences of at most `few` packed rows are cut by cut[0] and go to the kernels that stream keys past few rows; the
+  // others by cut[1], to the kernel whose wavefronts share key tiles.  cut[i].tiles is 0 where a class cannot occur.
+  int32_t few;
+  pt_paged_cut cut[2];
 };
 
-// How a batch is cut: rows (row, head of the group) per tile, upper bound of the number of tiles, keys per range.
 struct pt_paged_plan {
-  int32_t tile_rows, tiles, chunk, n_splits;
+  int32_t few;
+  pt_paged_cut cut[2];
   size_t off_ml, bytes;   // workspace: part_o first
 };
 
