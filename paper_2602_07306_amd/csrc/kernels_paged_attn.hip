@@ -14,7 +14,7 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lptr_t;
 typedef __attribute__((address_space(3))) s16x4_t* lptr4_t;
-typedef const __attribute__((address_space(1))) void* gptr_t;
+typedef const __attribute__((address_space(4))) int32_t* cptr_t;   // what no kernel writes: scalar loads
 
 constexpr int PA_MAX_SPLITS = 64;   // a wavefront of the combine holds one range's statistics per lane
 
@@ -194,6 +194,13 @@ struct paged_geom {
   static __device__ __forceinline__ int swz(int row) { return HD == 64 ? (row >> 1) & 7 : row & 15; }
 };
 
+// 16 bytes per lane from base + off into LDS, 1024 consecutive bytes from `lds` on.  Inline assembly because the compiler takes
+// any LDS read to depend on such a load of its own and waits for all of them in front of it, that is for the next tile in
+// front of this one's first product.  There are no result registers; every wait for these loads is written out.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+
 template <int HD, int NQ, bool FULL>
 __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -247,20 +254,28 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
     voff[i] = (uint32_t)(row * a.token_stride * 2 + c * 16);
     on[i] = FULL || c * 8 < a.hd;
   }
-  const int32_t* pages = a.b.pages + t.seq * a.b.pages_stride;
+  const cptr_t pages = (cptr_t)(a.b.pages + t.seq * a.b.pages_stride);
   const int mask = (1 << a.b.page_shift) - 1;
-  // lane j: page of the tile's j-th 16 keys (of the last key in the range where those are behind it)
-  auto page_ids = [&](int kb) { return pages[min(kb + 16 * (lane & (NB - 1)), k1 - 1) >> a.b.page_shift]; };
-  auto load_tile = [&](const void* cache, uint32_t lds, int kb, int pid) {
+  // pages of the tile's blocks of 16 keys (of the range's last key where those are behind it)
+  auto page_ids = [&](int kb, int (&id)[NB]) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) id[j] = pages[min(kb + 16 * j, k1 - 1) >> a.b.page_shift];
+  };
+  auto load_tile = [&](const void* cache, uint32_t lds, int kb, const int (&id)[NB]) {
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const int page = paged_checked(a.b, __builtin_amdgcn_readlane(pid, j));
+      const int page = (unsigned)id[j] < (unsigned)a.b.n_pages ? id[j] : 0;
       const char* base = (const char*)cache + (page * a.page_stride + ((kb + 16 * j) & mask) * a.token_stride + kvh * a.head_stride) * 2;
 #pragma unroll
       for (int i = 0; i < PER16; ++i)
-        if (on[i])
-          __builtin_amdgcn_global_load_lds((gptr_t)(base + voff[i]), (lptr_t)(uintptr_t)(lds + (j * PER16 + i) * 1024), 16, 0, 0);
+        if (on[i]) load_to_lds(lds + (j * PER16 + i) * 1024, base, voff[i]);
     }
+  };
+  auto report = [&](const int (&id)[NB]) {
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) bad |= (unsigned)id[j] >= (unsigned)a.b.n_pages;
+    if (bad) paged_raise(a.b, PT_PAGED_BAD_PAGE);
   };
 
   f32x4_t acc[NQ][HB];
@@ -274,13 +289,14 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
   }
   const float c_log2 = a.scale_log2;
   int kb = k0 + wave * TK;
-  int pid = 0;
+  int pid[NB];
   if (!FULL) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the zeros are in LDS
   if (kb < k1) {
-    pid = page_ids(kb);
+    page_ids(kb, pid);
     load_tile(a.kc, kt_lds, kb, pid);
     load_tile(a.vc, vt_lds, kb, pid);
-    pid = page_ids(min(kb + 4 * TK, k1 - 1));
+    report(pid);
+    page_ids(min(kb + 4 * TK, k1 - 1), pid);
   }
   for (; kb < k1; kb += 4 * TK) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the tile has landed; the wavefront is alone with it
@@ -321,7 +337,8 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) {
       load_tile(a.vc, vt_lds, kb + 4 * TK, pid);
-      pid = page_ids(min(kb + 8 * TK, k1 - 1));
+      report(pid);
+      page_ids(min(kb + 8 * TK, k1 - 1), pid);
     }
     if (tail) {   // cache bytes behind the range are not data: zeroed, so that 0 * x stays 0
 #pragma unroll
@@ -405,19 +422,12 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
 // bf16, many rows: four wavefronts of 32 packed rows each share key tiles of 64 (K and V as they lie in their pages, two
 // tiles in LDS: one that is read, one on its way).  A wavefront loads the tile's 16 keys of its number - one page - and
 // multiplies all 64 with its own rows; MFMA layouts, swizzle and transposing reads as above.
-// The loads to LDS are inline assembly: the compiler takes any LDS read to depend on such a load of its own and waits for
-// all of them in front of it, that is for the next tile in front of this one's first product.  They have no result
-// registers; what waits for them is written out below, one wait and one barrier per tile.
 // ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
-}
-
 template <int HD, bool FULL>
 __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_attn_args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using geo = paged_geom<HD>;
-  constexpr int TK = 64, CH = geo::CH, RPI = geo::RPI, PER16 = geo::PER16, TILE_B = geo::TILE_B, ROWB = geo::ROWB;
+  constexpr int TK = 64, CH = geo::CH, RPI = geo::RPI, PER16 = geo::PER16, ROWB = geo::ROWB, TILE_B = TK * ROWB;
   constexpr int NB = TK / 16, KS = HD / 32, HB = HD / 16, NU = TK / 32, NQ = 2;
   extern __shared__ __attribute__((aligned(1024))) char smem[];   // [2][K tile, V tile]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -467,7 +477,6 @@ __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_
     voff[i] = (uint32_t)(row * a.token_stride * 2 + c * 16);
     on[i] = FULL || c * 8 < a.hd;
   }
-  typedef const __attribute__((address_space(4))) int32_t* cptr_t;
   const cptr_t pages = (cptr_t)(a.b.pages + t.seq * a.b.pages_stride);
   const int mask = (1 << a.b.page_shift) - 1;
   // page of the wavefront's 16 keys of the tile (of the range's last key where those are behind it)
@@ -777,35 +786,34 @@ __global__ void __launch_bounds__(256, 1) paged_attn_f32_kernel(const pt_paged_a
   paged_merge<float, HD>(a, t, split, kvh, k0, k1, red_o, red_ml);
 }
 
-// Joins the ranges of one (row, head) per wavefront, in their order.  Rows whose keys fitted one range are done already.
-template <typename T>
+// Joins the ranges of a tile's rows, a row per wavefront at a time and in the ranges' order; 16 rows per workgroup.  Tiles whose
+// keys fitted one range are done already.
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) paged_combine_kernel(const pt_paged_attn_args a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int row = __builtin_amdgcn_readfirstlane((int)(unit / a.H)), head = __builtin_amdgcn_readfirstlane((int)(unit % a.H));
-  if (row >= a.b.total_rows) return;
-  const int seq = paged_find_row(a.b, row);
-  if (seq >= a.b.n_seqs) return;
-  const paged_seq sq = paged_load_seq(a.b, seq);
-  if (row < sq.first || row >= sq.first + sq.n) return;
-  const int G = a.H / a.Hkv;
-  const int i = row - sq.first;
-  const pt_paged_cut& cut = a.cut[paged_in_class<true>(a, sq.n)];
-  const int tile = (i * G + head % G) / cut.tile_rows;
-  const int64_t last = min((int64_t)(tile + 1) * cut.tile_rows, (int64_t)sq.n * G) - 1;
-  const int nsplit = (int)(((int64_t)paged_vis(a, sq, (int)(last / G)) + cut.chunk - 1) / cut.chunk);
-  if (nsplit <= 1) return;
-  const int64_t step = (int64_t)a.b.total_rows * a.H, at = (int64_t)row * a.H + head;
-  float2 ml = make_float2(-INFINITY, 0.f);
-  if (lane < nsplit) ml = a.part_ml[lane * step + at];
-  const float m = wave_max(ml.x);
-  const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-  const float l = wave_sum(f * ml.y);
-  const int lim = paged_vis(a, sq, i);
-  for (int e = lane; e < a.hd; e += 64) {
-    float o = 0.f;
-    for (int s = 0; s < nsplit; ++s) o += __shfl(f, s, 64) * a.part_o[(s * step + at) * a.hd + e];
-    elem<T>::st((T*)a.o + row * a.o_rs + head * a.o_hs + e, lim <= 0 ? 0.f : o / l);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const pt_paged_cut& cut = a.cut[WIDE];
+  const int parts = cut.tile_rows / 16, G = a.H / a.Hkv;
+  const int kvh = blockIdx.x % a.Hkv;
+  const int rest = blockIdx.x / a.Hkv;
+  paged_tile t;
+  if (!paged_find_tile<WIDE>(a, rest / parts, &t) || t.nsplit == 1) return;
+  const int r0 = rest % parts * 16;
+  const int64_t step = (int64_t)a.b.total_rows * a.H;
+  for (int r = r0 + wave; r < min(r0 + 16, t.nrows); r += 4) {
+    const int i = (t.row0 + r) / G, head = kvh * G + (t.row0 + r) - i * G, row = t.sq.first + i;
+    const int64_t at = (int64_t)row * a.H + head;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < t.nsplit) ml = a.part_ml[lane * step + at];
+    const float m = wave_max(ml.x);
+    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+    const float l = wave_sum(f * ml.y);
+    const int lim = paged_vis(a, t.sq, i);
+    for (int e = lane; e < a.hd; e += 64) {
+      float o = 0.f;
+#pragma unroll 4
+      for (int s = 0; s < t.nsplit; ++s) o += __shfl(f, s, 64) * a.part_o[(s * step + at) * a.hd + e];
+      elem<T>::st((T*)a.o + row * a.o_rs + head * a.o_hs + e, lim <= 0 ? 0.f : o / l);
+    }
   }
 }
 
@@ -824,8 +832,8 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
   if (rows_max > 0x3fffffff) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "max_q_len times the heads of a group is too large");
   const bool wide = dtype == PT_BF16 && hd <= 128 && rows_max > 32;
   // Blocks of 16 packed rows in a tile of the few-row kernels: what the longest sequence needs, or beside longer ones, what a
-  // single new row needs.
-  const int64_t few = wide ? (G <= 32 ? G : 0) : rows_max;
+  // single new row needs; none where a lone sequence is all there is.
+  const int64_t few = wide ? (G <= 32 && b.n_seqs > 1 ? G : 0) : rows_max;
   const int nq = dtype == PT_F32 || few <= 16 ? 1 : 2;
   p->cut[0].tile_rows = 16 * nq;
   p->few = wide ? (few > 0 ? 16 * nq : 0) : 0x7fffffff;
@@ -842,7 +850,7 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
   // enough ranges for 2048 workgroups, each of at least a tile for every wavefront
   if (t0 > 0) paged_ranges(t0 * Hkv, keys, 2048, 256, &p->cut[0]);
   if (t1 > 0) paged_ranges(t1 * Hkv, keys, 512, 256, &p->cut[1]);
-  if (t0 * Hkv * p->cut[0].n_splits > 0x7fffffff || t1 * Hkv * p->cut[1].n_splits > 0x7fffffff || (int64_t)b.total_rows * H > ((int64_t)1 << 32))
+  if (t0 * Hkv * std::max(2, p->cut[0].n_splits) > 0x7fffffff || t1 * Hkv * std::max(8, p->cut[1].n_splits) > 0x7fffffff)
     return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
   const int32_t splits = std::max(p->cut[0].n_splits, p->cut[1].n_splits);
   if (splits > 1) {
@@ -874,11 +882,17 @@ static int launch_paged_f32(const pt_paged_attn_args& a, unsigned grid, hipStrea
 
 template <int HD, bool FULL>
 static int launch_wide(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
-  constexpr int LDS = 4 * paged_geom<HD>::TILE_B;
+  constexpr int LDS = 4 * 64 * paged_geom<HD>::ROWB;
   auto kern = paged_attn_wide_kernel<HD, FULL>;
   PT_SET_MAX_LDS_ONCE(kern, LDS);
   hipLaunchKernelGGL(kern, dim3(grid), dim3(256), LDS, s, a);
   return PT_OK;
+}
+
+template <typename T, bool WIDE>
+static void launch_combine(const pt_paged_attn_args& a, hipStream_t s) {
+  const unsigned blocks = (unsigned)((int64_t)a.cut[WIDE].tiles * a.Hkv * (a.cut[WIDE].tile_rows / 16));
+  hipLaunchKernelGGL((paged_combine_kernel<T, WIDE>), dim3(blocks), dim3(256), 0, s, a);
 }
 
 int pt_launch_paged_attn(const pt_paged_attn_args& a, int32_t dtype, hipStream_t s) {
@@ -902,11 +916,10 @@ int pt_launch_paged_attn(const pt_paged_attn_args& a, int32_t dtype, hipStream_t
     }
   }
   if (rc) return rc;
-  if (std::max(a.cut[0].n_splits, a.cut[1].n_splits) > 1) {
-    const int64_t waves = (int64_t)a.b.total_rows * a.H;
-    const unsigned blocks = (unsigned)((waves + 3) / 4);
-    if (dtype == PT_F32) hipLaunchKernelGGL(paged_combine_kernel<float>, dim3(blocks), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(paged_combine_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, a);
+  if (a.cut[1].n_splits > 1) launch_combine<bf16_t, true>(a, s);
+  if (a.cut[0].n_splits > 1) {
+    if (dtype == PT_F32) launch_combine<float, false>(a, s);
+    else launch_combine<bf16_t, false>(a, s);
   }
   PT_HIP_CHECK(hipGetLastError());
   return PT_OK;
