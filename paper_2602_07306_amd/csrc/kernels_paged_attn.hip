@@ -6,6 +6,7 @@
 // four wavefronts take the range's key tiles in turn and are merged at the end through LDS.  Where one range does not hold all
 // keys, each leaves its unscaled sums and statistics to paged_combine_kernel.
 #include <algorithm>
+#include <type_traits>
 
 #include "pt_paged_device.h"
 
@@ -15,6 +16,22 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lptr_t;
 typedef __attribute__((address_space(3))) s16x4_t* lptr4_t;
 typedef const __attribute__((address_space(4))) int32_t* cptr_t;   // what no kernel writes: scalar loads
+
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (N > 0) {
+    static_for<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
+// Largest of the four lanes that share lane % 16.
+__device__ __forceinline__ float max_over_groups(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 
 constexpr int PA_MAX_SPLITS = 64;   // a wavefront of the combine holds one range's statistics per lane
 
@@ -191,14 +208,35 @@ struct paged_geom {
   static constexpr int RPI = 64 / CH;                 // rows per load instruction of 1024 bytes
   static constexpr int PER16 = 16 / RPI;              // load instructions per 16 keys
   static constexpr int TILE_B = TK * ROWB;
-  static __device__ __forceinline__ int swz(int row) { return HD == 64 ? (row >> 1) & 7 : row & 15; }
+  // XOR of a row's chunk numbers.  A 16-byte read of 16 rows at once must meet 16 different chunks (of 256 bytes), a
+  // transposing read of 8 rows at once 8 different pairs of chunks: the row's low bits choose the pair, a higher one the half.
+  static __device__ __forceinline__ int swz(int row) { return HD == 64 ? (row & 6) | (row >> 3 & 1) : (row & 7) << 1 | (row >> 3 & 1); }
 };
 
-// 16 bytes per lane from base + off into LDS, 1024 consecutive bytes from `lds` on.  Inline assembly because the compiler takes
-// any LDS read to depend on such a load of its own and waits for all of them in front of it, that is for the next tile in
-// front of this one's first product.  There are no result registers; every wait for these loads is written out.
-__device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+// 16 keys of a page into LDS at `lds`: N instructions of 1024 consecutive LDS bytes, 16 per lane, from base + off[i] + LDS_BIAS.
+// Instruction i's offset field counts for both sides, so off[i] is short of 1024 (i % 4) (and base of the bias that keeps
+// it positive); m0, the LDS address, is set once for four.  Inline assembly because the compiler takes any LDS read to
+// depend on such a load of its own and waits for all of them in front of it, that is for the next tile in front of this
+// one's first product.  There are no result registers; every wait for these loads is written out.
+constexpr int LDS_BIAS = 3072;
+template <int N, bool FULL>
+__device__ __forceinline__ void load_keys_to_lds(uint32_t lds, const char* base, const uint32_t (&off)[N], const bool (&on)[N]) {
+  if constexpr (FULL && N == 2) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024"
+                 ::"s"(lds), "v"(off[0]), "v"(off[1]), "s"(base) : "memory", "m0");
+  } else if constexpr (FULL) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+                   "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
+                   ::"s"(lds + i * 1024), "v"(off[i]), "v"(off[i + 1]), "v"(off[i + 2]), "v"(off[i + 3]), "s"(base) : "memory", "m0");
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (on[i])
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
+                     ::"s"(lds + i / 4 * 4096), "v"(off[i]), "s"(base), "n"(i % 4 * 1024) : "memory", "m0");
+  }
 }
 
 template <int HD, int NQ, bool FULL>
@@ -251,7 +289,7 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
 #pragma unroll
   for (int i = 0; i < PER16; ++i) {
     const int row = i * RPI + lane / CH, c = (lane % CH) ^ geo::swz(row);
-    voff[i] = (uint32_t)(row * a.token_stride * 2 + c * 16);
+    voff[i] = (uint32_t)(row * a.token_stride * 2 + c * 16) + LDS_BIAS - i % 4 * 1024;
     on[i] = FULL || c * 8 < a.hd;
   }
   const cptr_t pages = (cptr_t)(a.b.pages + t.seq * a.b.pages_stride);
@@ -261,14 +299,16 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
 #pragma unroll
     for (int j = 0; j < NB; ++j) id[j] = pages[min(kb + 16 * j, k1 - 1) >> a.b.page_shift];
   };
-  auto load_tile = [&](const void* cache, uint32_t lds, int kb, const int (&id)[NB]) {
+  const char* const k_base = (const char*)a.kc + kvh * a.head_stride * 2 - LDS_BIAS;
+  const char* const v_base = (const char*)a.vc + kvh * a.head_stride * 2 - LDS_BIAS;
+  const int64_t page_bytes = a.page_stride * 2;
+  const uint32_t token_bytes = (uint32_t)a.token_stride * 2;
+  auto load_tile = [&](const char* cache, uint32_t lds, int kb, const int (&id)[NB]) {
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const int page = (unsigned)id[j] < (unsigned)a.b.n_pages ? id[j] : 0;
-      const char* base = (const char*)cache + (page * a.page_stride + ((kb + 16 * j) & mask) * a.token_stride + kvh * a.head_stride) * 2;
-#pragma unroll
-      for (int i = 0; i < PER16; ++i)
-        if (on[i]) load_to_lds(lds + (j * PER16 + i) * 1024, base, voff[i]);
+      const uint32_t slot = ((kb + 16 * j) & mask) * token_bytes;   // page_size * token_stride < 2^31 elements
+      load_keys_to_lds<PER16, FULL>(lds + j * PER16 * 1024, cache + (page * page_bytes + slot), voff, on);
     }
   };
   auto report = [&](const int (&id)[NB]) {
@@ -293,8 +333,8 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
   if (!FULL) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the zeros are in LDS
   if (kb < k1) {
     page_ids(kb, pid);
-    load_tile(a.kc, kt_lds, kb, pid);
-    load_tile(a.vc, vt_lds, kb, pid);
+    load_tile(k_base, kt_lds, kb, pid);
+    load_tile(v_base, vt_lds, kb, pid);
     report(pid);
     page_ids(min(kb + 4 * TK, k1 - 1), pid);
   }
@@ -310,7 +350,7 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
         kf[b][kk] = *(const bf16x8_t*)(kt + row * geo::ROWB + (((kk * 4 + g) ^ geo::swz(row)) * 16));
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) load_tile(a.kc, kt_lds, kb + 4 * TK, pid);
+    if (more) load_tile(k_base, kt_lds, kb + 4 * TK, pid);
     f32x4_t s[NQ][NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -336,7 +376,7 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
         }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (more) {
-      load_tile(a.vc, vt_lds, kb + 4 * TK, pid);
+      load_tile(v_base, vt_lds, kb + 4 * TK, pid);
       report(pid);
       page_ids(min(kb + 8 * TK, k1 - 1), pid);
     }
@@ -366,8 +406,7 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[n][b][v]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      mx = max_over_groups(mx);
       const float m_new = fmaxf(m_run[n], mx);
       const float ref = m_new == -INFINITY ? 0.f : m_new;   // no key seen yet
       const float corr = __builtin_amdgcn_exp2f((m_run[n] - ref) * c_log2);
@@ -429,7 +468,7 @@ __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_
   using geo = paged_geom<HD>;
   constexpr int TK = 64, CH = geo::CH, RPI = geo::RPI, PER16 = geo::PER16, ROWB = geo::ROWB, TILE_B = TK * ROWB;
   constexpr int NB = TK / 16, KS = HD / 32, HB = HD / 16, NU = TK / 32, NQ = 2;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [2][K tile, V tile]
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [2][K tile], [2][V tile]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const int kvh = blockIdx.x % a.Hkv;
@@ -474,28 +513,26 @@ __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_
 #pragma unroll
   for (int i = 0; i < PER16; ++i) {
     const int row = i * RPI + lane / CH, c = (lane % CH) ^ geo::swz(row);
-    voff[i] = (uint32_t)(row * a.token_stride * 2 + c * 16);
+    voff[i] = (uint32_t)(row * a.token_stride * 2 + c * 16) + LDS_BIAS - i % 4 * 1024;
     on[i] = FULL || c * 8 < a.hd;
   }
   const cptr_t pages = (cptr_t)(a.b.pages + t.seq * a.b.pages_stride);
   const int mask = (1 << a.b.page_shift) - 1;
   // page of the wavefront's 16 keys of the tile (of the range's last key where those are behind it)
   auto page_id = [&](int kb) { return pages[min(kb + 16 * wave, k1 - 1) >> a.b.page_shift]; };
-  auto load_tile = [&](int kb, int page, uint32_t stage) {
+  const char* const k_base = (const char*)a.kc + kvh * a.head_stride * 2 - LDS_BIAS;
+  const char* const v_base = (const char*)a.vc + kvh * a.head_stride * 2 - LDS_BIAS;
+  const int64_t page_bytes = a.page_stride * 2;
+  const uint32_t token_bytes = (uint32_t)a.token_stride * 2;
+  const uint32_t lds_wave = lds0 + wave * 16 * ROWB;
+  // where the wavefront's 16 keys of the tile lie, in K as in V
+  auto offset_of = [&](int kb, int page) {
     if ((unsigned)page >= (unsigned)a.b.n_pages) {
       paged_raise(a.b, PT_PAGED_BAD_PAGE);
       page = 0;
     }
-    const int64_t at = (page * a.page_stride + ((kb + 16 * wave) & mask) * a.token_stride + kvh * a.head_stride) * 2;
-    const char* k = (const char*)a.kc + at;
-    const char* v = (const char*)a.vc + at;
-    const uint32_t lds = lds0 + stage + wave * 16 * ROWB;
-#pragma unroll
-    for (int i = 0; i < PER16; ++i)
-      if (on[i]) load_to_lds(lds + i * 1024, k, voff[i]);
-#pragma unroll
-    for (int i = 0; i < PER16; ++i)
-      if (on[i]) load_to_lds(lds + TILE_B + i * 1024, v, voff[i]);
+    const uint32_t slot = ((kb + 16 * wave) & mask) * token_bytes;   // page_size * token_stride < 2^31 elements
+    return page * page_bytes + slot;
   };
 
   // LDS addresses of the fragments of the first 16 keys
@@ -504,7 +541,7 @@ __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_
   for (int kk = 0; kk < KS; ++kk) ka[kk] = lds0 + l16 * ROWB + (((kk * 4 + g) ^ geo::swz(l16)) * 16);
   const int vrow = 4 * g + (l16 >> 2);
 #pragma unroll
-  for (int hb = 0; hb < HB; ++hb) va[hb] = lds0 + TILE_B + vrow * ROWB + (((hb * 2 + ((l16 & 3) >> 1)) ^ geo::swz(vrow)) * 16) + (l16 & 1) * 8;
+  for (int hb = 0; hb < HB; ++hb) va[hb] = lds0 + 2 * TILE_B + vrow * ROWB + (((hb * 2 + ((l16 & 3) >> 1)) ^ geo::swz(vrow)) * 16) + (l16 & 1) * 8;
   typedef const __attribute__((address_space(3))) bf16x8_t* lk_t;
 
   f32x4_t acc[NQ][HB];
@@ -517,107 +554,207 @@ __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_
     for (int hb = 0; hb < HB; ++hb) acc[n][hb] = {0.f, 0.f, 0.f, 0.f};
   }
   const float c_log2 = a.scale_log2;
+  constexpr uint32_t K_STAGE = TILE_B, V_LDS = 2 * TILE_B;
+  constexpr int UK = 32, UB = UK / 16;        // keys of a unit, in blocks of 16
+  constexpr int NS = UB * KS, STEPS = NS + HB;   // operand fragments of a unit: K's, then those of V^T; each feeds NQ MFMAs
+  constexpr int PF = 4;                       // fragments in flight between LDS and their MFMAs
+  union frag {
+    s16x4_t h[2];
+    bf16x8_t v;
+  };
+  // s[n][b], register v: key first + 16 b + 4 g + v, query n * 16 + l16
+  auto mask_unit = [&](f32x4_t (&s)[NQ][UB], int first) __attribute__((always_inline)) {
+    if (first + UK > lim_first) {
+      int key = first + 4 * g;
+      asm volatile("" : "+v"(key));   // the keys' numbers are formed here and not in front of the branch
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int b = 0; b < UB; ++b)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (key + 16 * b + v >= lim[n]) s[n][b][v] = -INFINITY;
+    }
+  };
+  // The reference of the exponentials is a whole binary order, and moves only when the maximum exceeds it by more than 8:
+  // until then the probabilities stay below 2^8, which fp32 sums and bf16 operands hold as well.  Moving it multiplies
+  // by a power of two, which is exact, for the probabilities (p) that wait for their product too.
+  union prob {
+    uint32_t u[4];
+    bf16x8_t v;
+  };
+  auto new_reference = [&](const float (&top)[NQ], prob (&p)[NQ]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const float mx = max_over_groups(top[n]) * c_log2;
+      const bool grow = mx > m_run[n] + 8.0f;
+      if (__any(grow)) {
+        const float m_new = grow ? ceilf(mx) : m_run[n];
+        const float corr = grow ? __builtin_amdgcn_exp2f(m_run[n] - m_new) : 1.0f;
+        m_run[n] = m_new;
+        l_run[n] *= corr;
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb) acc[n][hb] *= corr;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[n].u[j] = pack_bf16x2(__uint_as_float(p[n].u[j] << 16) * corr, __uint_as_float(p[n].u[j] & 0xffff0000u) * corr);
+      }
+    }
+  };
+  // Fragment f of a unit into its place of the ring.  K's come block by block of keys inside a step of the head, so that four
+  // chains of sums alternate.
+  frag fr[PF];
+  auto fetch = [&](auto F_, uint32_t k_at, uint32_t v_at) __attribute__((always_inline)) {
+    constexpr int f = decltype(F_)::value;
+    if constexpr (f < NS) {
+      fr[f % PF].v = *(lk_t)(uintptr_t)(ka[f / UB] + k_at + (f % UB) * 16 * ROWB);
+    } else {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) fr[f % PF].h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr4_t)(uintptr_t)(va[f - NS] + v_at + 16 * x * ROWB));
+    }
+  };
+  static_assert(STEPS % PF == 0 && NS % PF == 0, "a unit begins at the ring's first place");
+  auto fill = [&](uint32_t k_at) __attribute__((always_inline)) { static_for<PF>([&](auto F_) { fetch(F_, k_at, 0); }); };
+  // Unit i of 32 keys: its probabilities p_new from its scores s_cur, beside two products that do not depend on them: the
+  // scores s_nxt of unit i + 1 and the values of unit i - 1 (p_old; LAG: there is one).  So matrix and vector pipes work
+  // side by side inside one wavefront.  k_at, v_at: LDS offsets of the two units; the ring holds the first fragments of
+  // K, and with NEXT receives those of the unit at k_next at the end.
+  auto unit = [&](auto LAG_, auto NEXT_, f32x4_t (&s_cur)[NQ][UB], f32x4_t (&s_nxt)[NQ][UB], prob (&p_old)[NQ], prob (&p_new)[NQ], uint32_t k_at,
+                  uint32_t v_at, uint32_t k_next, int first) __attribute__((always_inline)) {
+    constexpr bool LAG = decltype(LAG_)::value, NEXT = decltype(NEXT_)::value;
+    constexpr int END = LAG ? STEPS : NS;
+    float mc[NQ], top[NQ], psum[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      mc[n] = m_run[n] == -INFINITY ? 0.f : m_run[n];
+      top[n] = -INFINITY;
+      psum[n] = 0.f;
+    }
+    // One MFMA at a time, and behind it its share of the scores: what a wavefront issues right behind an MFMA runs beside it,
+    // another MFMA would wait for the first one's end.
+    constexpr int SCORES = NQ * UB * 4, SLOTS = END * NQ;
+    float half[NQ];
+    static_for<SLOTS>([&](auto I_) {
+      constexpr int slot = decltype(I_)::value, i = slot / NQ, n = slot % NQ;
+      if constexpr (i < NS) {
+        constexpr int b = i % UB, kk = i / UB;
+        if (kk == 0) s_nxt[n][b] = {0.f, 0.f, 0.f, 0.f};
+        s_nxt[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i % PF].v, qf[n][kk], s_nxt[n][b], 0, 0, 0);
+      } else {
+        acc[n][i - NS] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i % PF].v, p_old[n].v, acc[n][i - NS], 0, 0, 0);
+      }
+      if constexpr (n == NQ - 1 && i + PF < END) fetch(std::integral_constant<int, i + PF>{}, k_at, v_at);
+      if constexpr (n == NQ - 1 && i + PF >= END && NEXT) fetch(std::integral_constant<int, i + PF - END>{}, k_next, 0);
+      static_for<SCORES>([&](auto J_) {
+        constexpr int sc = decltype(J_)::value;
+        if constexpr (sc * SLOTS / SCORES == slot) {   // score: query block, key block, register
+          constexpr int n = sc / (UB * 4), b = sc / 4 % UB, v = sc % 4;
+          float p = __builtin_amdgcn_exp2f(fmaf(s_cur[n][b][v], c_log2, -mc[n]));
+          psum[n] += p;
+          // formed here: the compiler would move all of it behind the last product otherwise
+          if constexpr (v % 2 == 0) {
+            asm volatile("" : "+v"(p), "+v"(psum[n]));
+            half[n] = p;
+          } else {
+            p_new[n].u[2 * b + v / 2] = pack_bf16x2(half[n], p);
+            asm volatile("" : "+v"(p_new[n].u[2 * b + v / 2]), "+v"(psum[n]));
+          }
+        }
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    mask_unit(s_nxt, first + UK);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      l_run[n] += psum[n];
+#pragma unroll
+      for (int b = 0; b < UB; ++b)
+#pragma unroll
+        for (int v = 0; v < 4; v += 2) top[n] = fmaxf(fmaxf(top[n], s_nxt[n][b][v]), s_nxt[n][b][v + 1]);
+    }
+    new_reference(top, p_new);
+  };
+
+  // Tile i of the range (two units): K in stage i % 2 of the first half of LDS, V in stage i % 2 of the second; K runs a
+  // unit ahead and V a unit behind, so tile i + 1 of K and tile i of V are needed together.
+  const int n_tiles = (k1 - k0 + TK - 1) / TK;
+  const int own = (max(lim_last - k0, 0) + UK - 1) / UK;   // units that this wavefront's rows see
   if (!FULL) __syncthreads();   // the zeros are in LDS
-  uint32_t stage = 0;
-  int next_page = 0;
-  if (k0 < k1) {
-    load_tile(k0, page_id(k0), 0);
-    next_page = page_id(min(k0 + TK, k1 - 1));
+  int page = 0;                 // of tile i + 2
+  int64_t v_off = 0;            // of tile i + 1
+  if (n_tiles > 0) {
+    const int64_t off = offset_of(k0, page_id(k0));
+    load_keys_to_lds<PER16, FULL>(lds_wave, k_base + off, voff, on);
+    load_keys_to_lds<PER16, FULL>(lds_wave + V_LDS, v_base + off, voff, on);
+    if (n_tiles > 1) {
+      v_off = offset_of(k0 + TK, page_id(k0 + TK));
+      load_keys_to_lds<PER16, FULL>(lds_wave + K_STAGE, k_base + v_off, voff, on);
+    }
+    page = page_id(min(k0 + 2 * TK, k1 - 1));
   }
-  for (int kb = k0; kb < k1; kb += TK) {
-    // this tile's loads are done, here and in the other wavefronts; nobody reads the other stage any more
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    if (kb + TK < k1) {
-      load_tile(kb + TK, next_page, stage ^ (2 * TILE_B));
-      next_page = page_id(min(kb + 2 * TK, k1 - 1));
-    } else if (kb + TK > k1) {
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  f32x4_t s_a[NQ][UB], s_b[NQ][UB];
+  prob p_a[NQ], p_b[NQ];
+  if (own > 0) {
+    float top[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int b = 0; b < UB; ++b) s_a[n][b] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const bf16x8_t kf = *(lk_t)(uintptr_t)(ka[i % KS] + (i / KS) * 16 * ROWB);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) s_a[n][i / KS] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][i % KS], s_a[n][i / KS], 0, 0, 0);
+    }
+    mask_unit(s_a, k0);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      top[n] = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p_b[n].u[j] = 0;
+#pragma unroll
+      for (int b = 0; b < UB; ++b)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) top[n] = fmaxf(top[n], s_a[n][b][v]);
+    }
+    new_reference(top, p_b);
+    // unit 0: nothing lags behind it
+    fill(UK * ROWB);
+    unit(std::false_type{}, std::false_type{}, s_a, s_b, p_b, p_a, UK * ROWB, 0, 0, k0);
+  }
+  auto tile = [&](auto ODD_, int i) __attribute__((always_inline)) {
+    constexpr uint32_t odd = decltype(ODD_)::value * K_STAGE;
+    // everything that was asked for is there, here and in the other wavefronts, and nobody reads K of tile i or V of tile
+    // i - 1 any more
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const int kb = k0 + i * TK;
+    fill(K_STAGE - odd);
+    if (i + 1 < n_tiles) load_keys_to_lds<PER16, FULL>(lds_wave + V_LDS + K_STAGE - odd, v_base + v_off, voff, on);
+    if (i + 2 < n_tiles) {
+      v_off = offset_of(kb + 2 * TK, page);
+      load_keys_to_lds<PER16, FULL>(lds_wave + odd, k_base + v_off, voff, on);
+      page = page_id(min(kb + 3 * TK, k1 - 1));
+    }
+    if (kb + TK > k1) {
       // positions behind the range are not data: their values become 0, so that 0 * x stays 0
-      for (int i = (k1 - kb) * CH + tid; i < TK * CH; i += 256) ((uint4*)(smem + stage + TILE_B))[i] = make_uint4(0, 0, 0, 0);
+      for (int j = (k1 - kb) * CH + tid; j < TK * CH; j += 256) ((uint4*)(smem + V_LDS + odd))[j] = make_uint4(0, 0, 0, 0);
       __syncthreads();
     }
-    if (kb < lim_last) {   // wavefront-uniform: some row sees some key of the tile
-      f32x4_t s[NQ][NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-#pragma unroll
-        for (int kk = 0; kk < KS; ++kk) {
-          const bf16x8_t kf = *(lk_t)(uintptr_t)(ka[kk] + stage + b * 16 * ROWB);
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            if (kk == 0) s[n][b] = {0.f, 0.f, 0.f, 0.f};
-            s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][kk], s[n][b], 0, 0, 0);
-          }
-        }
-      }
-      union {
-        uint32_t u[4];
-        bf16x8_t v;
-      } pf[NQ][NU];
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        if (kb + TK > lim_first) {
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-              if (kb + 16 * b + 4 * g + v >= lim[n]) s[n][b][v] = -INFINITY;
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) mx = fmaxf(mx, s[n][b][v]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        // The reference of the exponentials moves only when the maximum exceeds it by more than 8 binary orders; until
-        // then the probabilities stay below 2^8, which fp32 sums and bf16 operands hold as well, and nothing is rescaled.
-        const bool grow = (mx - m_run[n]) * c_log2 > 8.0f;
-        if (__any(grow)) {
-          const float m_new = grow ? mx : m_run[n];
-          const float corr = grow ? __builtin_amdgcn_exp2f((m_run[n] - m_new) * c_log2) : 1.0f;
-          m_run[n] = m_new;
-          l_run[n] *= corr;
-#pragma unroll
-          for (int hb = 0; hb < HB; ++hb) acc[n][hb] *= corr;
-        }
-        const float mc = m_run[n] == -INFINITY ? 0.f : m_run[n] * c_log2;
-        float psum = 0.f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            s[n][b][v] = __builtin_amdgcn_exp2f(fmaf(s[n][b][v], c_log2, -mc));
-            psum += s[n][b][v];
-          }
-        l_run[n] += psum;
-#pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) pf[n][u].u[j] = pack_bf16x2(s[n][2 * u + (j >> 1)][2 * (j & 1)], s[n][2 * u + (j >> 1)][2 * (j & 1) + 1]);
-      }
-#pragma unroll
-      for (int hb = 0; hb < HB; ++hb)
-#pragma unroll
-        for (int u = 0; u < NU; ++u) {
-          union {
-            s16x4_t h[2];
-            bf16x8_t v;
-          } vf;
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-            vf.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr4_t)(uintptr_t)(va[hb] + stage + (32 * u + 16 * x) * ROWB));
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) acc[n][hb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[n][u].v, acc[n][hb], 0, 0, 0);
-        }
-    }
-    stage ^= 2 * TILE_B;
+    // units 2 i + 1 and 2 i + 2; past the wavefront's own, scores are masked whatever LDS holds, and one unit more takes the
+    // last product
+    if (2 * i + 1 <= own) unit(std::true_type{}, std::true_type{}, s_b, s_a, p_a, p_b, K_STAGE - odd, odd, K_STAGE - odd + UK * ROWB, kb + UK);
+    if (2 * i + 2 <= own) unit(std::true_type{}, std::false_type{}, s_a, s_b, p_b, p_a, K_STAGE - odd + UK * ROWB, odd + UK * ROWB, 0, kb + TK);
+  };
+  for (int i = 0; i < n_tiles; i += 2) {   // two stages: their addresses are constants
+    tile(std::integral_constant<uint32_t, 0>{}, i);
+    if (i + 1 < n_tiles) tile(std::integral_constant<uint32_t, 1>{}, i + 1);
   }
   // acc[n][hb], register v: element 16 hb + 4 g + v of query n * 16 + l16
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     float l = l_run[n] + __shfl_xor(l_run[n], 16, 64);
     l += __shfl_xor(l, 32, 64);
-    const float m = m_run[n] * c_log2;
+    const float m = m_run[n];
     const int r = t.row0 + w0 + n * 16 + l16, i = r / G, head = kvh * G + (r - i * G), row = t.sq.first + i;
     const bool real = w0 + n * 16 + l16 < t.nrows;
     const int see = paged_vis(a, t.sq, i);
@@ -746,8 +883,7 @@ __global__ void __launch_bounds__(256, 1) paged_attn_f32_kernel(const pt_paged_a
         if (kb + 4 * g + v >= lim) s[v] = -INFINITY;
     }
     float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    mx = max_over_groups(mx);
     const float m_new = fmaxf(m_run, mx);
     const float ref = m_new == -INFINITY ? 0.f : m_new;
     const float corr = __builtin_amdgcn_exp2f((m_run - ref) * c_log2);
