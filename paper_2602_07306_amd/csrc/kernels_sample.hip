@@ -1,7 +1,7 @@
 // Sampling one token per row of logits: temperature, top-k, top-p, min-p, inverse of the running sum in order of index.
 //
 // One workgroup per row.  Weights w = exp((x - max) / T) are formed in fp64 (its products run at the rate of unpacked fp32
-// ones on this chip) and held as integers of 2^-S with S = 62 - ceil(log2 vocab), at most 52: sums of integers do not depend
+// ones on this chip) and held as integers of 2^-S with S = 62 - ceil(log2 vocab), at most 51: sums of integers do not depend
 // on their order, so atomics, reductions and scans may run in any, and a row's answer is a function of its inputs alone.
 // The kept set of top-k and top-p is a prefix of the order (logit descending, index ascending), so it is described by
 // its last element; no filter ever sorts a row.
@@ -11,12 +11,19 @@
 //     kept element, its members are gathered and sorted; where they do not fit, further histograms split its range of keys.
 //   pick: sixteen wavefronts sum a sixteenth of the range each, the one that holds the target is split again.
 // Rows are read from HBM once and from the caches in the later passes.
+// Few rows of many logits leave most of the chip idle and one compute unit with all fp64 work of a row: their rows are cut
+// into parts first (sample_part_kernel), whose workgroups find each part's largest logit, its wavefronts' sums of weights relative
+// to that, or its candidates for top-k; sample_kernel then starts from those.
+#include <algorithm>
+
 #include "pt_device.h"
 #include "pt_serving.h"
 
 typedef unsigned long long u64;
 
 constexpr int SAMPLE_BINS = 2048;
+constexpr int SAMPLE_U = 1;           // loads in flight of a thread where it forms weights
+
 constexpr int SAMPLE_LIST = 2048;     // gathered elements that fit
 constexpr int SAMPLE_LIST_K = 640;    // top-k by gathering: past it 1024 group maxima leave more than the list holds
 constexpr uint32_t KEY_NEG_INF = 0x007fffffu;
@@ -28,6 +35,18 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+
+constexpr int SAMPLE_PARTS = 16;      // of a row at most
+constexpr int SAMPLE_PART_K = 192;    // top-k by a part's candidates up to here
+constexpr int SAMPLE_PART_LIST = 512; // candidates of a part that fit
+
+// What a part leaves for the row's workgroup.
+struct sample_part {
+  float max, min;            // largest logit, smallest finite one
+  int n, pad;                // candidates found (more than fit: none are there); -1: not asked for
+  u64 sum[16];               // weights of each wavefront's stretch, relative to max
+  u64 list[SAMPLE_PART_LIST];
+};
 
 struct sample_lds {
   u64 list[SAMPLE_LIST];       // histogram or gathered elements (inverted key, index)
@@ -43,51 +62,59 @@ struct sample_lds {
 struct sample_row {
   const float* x;
   int V, S;
-  float max;
+  float max, top;              // largest logit; the same, or 0 where that is infinite and only its equals count
+  bool infinite;
   double c;                    // log2 e / T
+  double rounder;              // 1.5 * 2^(52 - S)
   uint32_t tau, tau_idx;       // last element kept by top-k and top-p
   u64 least;                   // min-p as a weight
   float bin_scale;
 
-  // weight of a logit, as an integer of 2^-S
-  __device__ __forceinline__ u64 weight(float v) const {
-    if (v == max) return (u64)1 << S;
-    if (!(v > -INFINITY) || max == INFINITY) return 0;
-    const double t = fmax(((double)v - (double)max) * c, -200.0);
-    const double n = rint(t);
-    const double r = (t - n) * 0.6931471805599453;   // exp(r) by its series, |r| <= 0.347: 6e-15
-    double p = 1.0 / 39916800;
-    p = fma(p, r, 1.0 / 3628800);
-    p = fma(p, r, 1.0 / 362880);
-    p = fma(p, r, 1.0 / 40320);
-    p = fma(p, r, 1.0 / 5040);
-    p = fma(p, r, 1.0 / 720);
-    p = fma(p, r, 1.0 / 120);
-    p = fma(p, r, 1.0 / 24);
-    p = fma(p, r, 1.0 / 6);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    return (u64)(ldexp(p, (int)n + S) + 0.5);
+  // Weight of a logit, as an integer of 2^-S; 0 for -infinity and NaN.  2^t with t = n + f, |f| <= 1/2: the polynomial of degree
+  // 9 through 2^f's values at Chebyshev's nodes, its constant term 1 (relative error 4e-14), n added to the exponent.  Whole
+  // numbers come out of sums with 1.5 * 2^k, whose low bits they are: n with k = 52, the weight with k = 52 - S.
+  __device__ __forceinline__ double power(float v) const {
+    const float x = v == max ? top : infinite ? -INFINITY : v;
+    const double t = fmax(((double)x - (double)top) * c, -200.0);   // the clamp also takes NaN: -infinity times 0
+    const double shifted = t + 6755399441055744.0;
+    const double f = t - (shifted - 6755399441055744.0);
+    double p = 1.0203121113055101e-07;
+    p = fma(p, f, 1.3255224878933224e-06);
+    p = fma(p, f, 1.5252686846120593e-05);
+    p = fma(p, f, 0.00015403455852451632);
+    p = fma(p, f, 0.0013333558179043103);
+    p = fma(p, f, 0.0096181291594025619);
+    p = fma(p, f, 0.055504108664760424);
+    p = fma(p, f, 0.24022650695812989);
+    p = fma(p, f, 0.69314718055994529);
+    p = fma(p, f, 1.0);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(shifted) << 20), __double2loint(p));
+  }
+  __device__ __forceinline__ u64 weight(float v) const { return (u64)__double_as_longlong(power(v) + rounder) - (u64)__double_as_longlong(rounder); }
+  __device__ __forceinline__ void set_max(float m) {
+    max = m;
+    infinite = m == INFINITY;
+    top = infinite ? 0.0f : m;
   }
   __device__ __forceinline__ bool in_prefix(uint32_t key, uint32_t i) const { return key > tau || (key == tau && i <= tau_idx); }
   __device__ __forceinline__ int bin(float v) const { return (int)fminf((max - v) * bin_scale, (float)(SAMPLE_BINS - 1)); }
 };
 
-// f(index, logit) for the elements lo .. hi-1, by `threads` threads, 16 bytes at a time whatever the row's alignment.
-template <typename F>
+// f(index, logit) for the elements lo .. hi-1, by `threads` threads, 16 bytes at a time whatever the row's alignment.  U loads
+// of a thread are in flight, and U * 4 calls run interleaved where they are free of branches.
+template <int U, typename F>
 __device__ __forceinline__ void for_each(const float* x, int lo, int hi, int tid, int threads, F&& f) {
   const int head = min(hi, lo + (int)((16 - ((uintptr_t)(x + lo) & 15)) >> 2 & 3));
-  if (lo + tid < head) f(lo + tid, x[lo + tid]);
   const int n4 = (hi - head) >> 2;
   const float4* x4 = (const float4*)(x + head);
-  for (int j0 = tid; j0 < n4; j0 += 4 * threads) {
-    float4 v[4];
+#pragma unroll 1
+  for (int j0 = tid; j0 < n4; j0 += U * threads) {
+    float4 v[U];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < U; ++u)
       if (j0 + u * threads < n4) v[u] = x4[j0 + u * threads];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < U; ++u) {
       if (j0 + u * threads < n4) {
         const int i = head + 4 * (j0 + u * threads);
         f(i, v[u].x);
@@ -97,8 +124,10 @@ __device__ __forceinline__ void for_each(const float* x, int lo, int hi, int tid
       }
     }
   }
+  // up to three elements in front of the 16-byte boundary, and up to three behind the last: one call
   const int done = head + 4 * n4;
-  if (done + tid < hi) f(done + tid, x[done + tid]);
+  int i = lo + tid < head ? lo + tid : tid >= 4 && done + tid - 4 < hi ? done + tid - 4 : -1;
+  if (i >= 0) f(i, x[i]);
 }
 
 __device__ __forceinline__ u64 wave_sum64(u64 v) {
@@ -113,6 +142,19 @@ __device__ __forceinline__ u64 wave_scan64(u64 v) {   // inclusive
     const u64 up = (u64)__shfl_up((long long)v, o, 64);
     if (lane >= o) v += up;
   }
+  return v;
+}
+// The wavefront's values in ascending order of lanes.
+__device__ __forceinline__ u64 wave_sort64(u64 v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int k = 2; k <= 64; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      const u64 o = (u64)__shfl_xor((long long)v, j, 64);
+      const bool low = (lane & j) == 0, up = (lane & k) == 0;
+      v = (v < o) == (low == up) ? v : o;
+    }
   return v;
 }
 // Inclusive sum over the workgroup's threads; *total the whole.
@@ -133,18 +175,18 @@ __device__ __forceinline__ u64 block_scan64(sample_lds& s, u64 v, u64* total) {
   return before + v;
 }
 
-// Smallest index i at which the running sum of weight(i, logit) exceeds `target(total)`; -1 where the total is 0.
+// Smallest index i at which the running sum of weight(i, logit) exceeds `target(total)`; -1 where the total is 0.  The
+// weights are free of branches: sixteen of a thread's run interleaved, where one alone is a chain of twenty dependent
+// fp64 operations (130001 weights of a row: 50 us with a branch in front of each, 30 us without).
+// The range lo .. hi-1 only, and with `known` for the target t.
 template <typename W, typename T>
-__device__ int sample_pick(sample_lds& s, const sample_row& r, W&& weight, T&& target) {
+__device__ int sample_pick_in(sample_lds& s, const sample_row& r, int lo, int hi, bool known, u64 t, W&& weight, T&& target) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int lo = 0, hi = r.V;
-  u64 t = 0;
-  bool known = false;
   while (!known || hi - lo > 1024) {
     const int part = ((hi - lo + 15) / 16 + 255) / 256 * 256;   // whole loads of a wavefront, until the end
     const int a = min(hi, lo + wave * part), b = min(hi, a + part);
     u64 sum = 0;
-    for_each(r.x, a, b, lane, 64, [&](int i, float v) { sum += weight(i, v); });
+    for_each<SAMPLE_U>(r.x, a, b, lane, 64, [&](int i, float v) { sum += weight(i, v); });
     sum = wave_sum64(sum);
     __syncthreads();
     if (lane == 0) s.wave[wave] = sum;
@@ -177,6 +219,10 @@ __device__ int sample_pick(sample_lds& s, const sample_row& r, W&& weight, T&& t
   __syncthreads();
   return found;
 }
+template <typename W, typename T>
+__device__ int sample_pick(sample_lds& s, const sample_row& r, W&& weight, T&& target) {
+  return sample_pick_in(s, r, 0, r.V, false, 0, weight, target);
+}
 
 // Sorts s.list[0 .. n-1] ascending; padded to a power of two with the largest value.
 __device__ void sample_sort(sample_lds& s, int n) {
@@ -196,13 +242,44 @@ __device__ void sample_sort(sample_lds& s, int n) {
   __syncthreads();
 }
 
+// A lower bound of the k-th largest logit of a range, k <= SAMPLE_LIST_K: the k-th largest of the maxima that its threads left in
+// s.tmax.  256 groups of them (about k (1 + k / 512) logits lie above the bound) are ranked by comparing each with all,
+// 1024 are sorted.
+__device__ float sample_bound(sample_lds& s, int k) {
+  const int tid = threadIdx.x;
+  if (k > 192) {
+    s.list[tid] = (u64)~key_of(s.tmax[tid]) << 32;
+    sample_sort(s, 1024);
+    return of_key(~(uint32_t)(s.list[k - 1] >> 32));
+  }
+  float gm = -INFINITY;
+  if (tid < 256) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) gm = fmaxf(gm, s.tmax[tid + 256 * j]);
+  }
+  __syncthreads();
+  if (tid < 256) s.tmax[tid] = gm;
+  __syncthreads();
+  if (tid < 256) {
+    int rank = 0;
+#pragma unroll 16
+    for (int j = 0; j < 256; ++j) {
+      const float o = s.tmax[j];
+      rank += o > gm || (o == gm && j < tid);
+    }
+    if (rank == k - 1) s.wmin[0] = gm;
+  }
+  __syncthreads();
+  return s.wmin[0];
+}
+
 // Gathers the elements that `take` accepts; their number (the list holds them only if it is at most SAMPLE_LIST).
 template <typename F>
-__device__ int sample_gather(sample_lds& s, const sample_row& r, F&& take) {
+__device__ int sample_gather(sample_lds& s, const sample_row& r, int lo, int hi, F&& take) {
   __syncthreads();
   if (threadIdx.x == 0) s.n = 0;
   __syncthreads();
-  for_each(r.x, 0, r.V, threadIdx.x, 1024, [&](int i, float v) {
+  for_each<4>(r.x, lo, hi, threadIdx.x, 1024, [&](int i, float v) {
     if (take(i, v)) {
       const int at = atomicAdd(&s.n, 1);
       if (at < SAMPLE_LIST) s.list[at] = (u64)~key_of(v) << 32 | (uint32_t)i;
@@ -212,16 +289,17 @@ __device__ int sample_gather(sample_lds& s, const sample_row& r, F&& take) {
   return s.n;
 }
 
-// Bin of s.list (as a histogram) in which the running sum reaches `target`; *before the sum in front of it.  -1: never.
-__device__ int sample_find_bin(sample_lds& s, u64 target, u64* before) {
+// Bin of a histogram, of which each thread holds two (a, b), in which the running sum reaches target(whole sum), which *need
+// receives; *before the sum in front of it.  -1: never.
+template <typename T>
+__device__ int sample_find_bin(sample_lds& s, u64 a, u64 b, T&& target_of, u64* need, u64* before) {
   const int tid = threadIdx.x;
-  __syncthreads();
-  const u64 a = s.list[2 * tid], b = s.list[2 * tid + 1];
   u64 total;
   const u64 c = block_scan64(s, a + b, &total);
   if (threadIdx.x == 0) s.found = -1;
   __syncthreads();
-  const u64 start = c - a - b;
+  const u64 start = c - a - b, target = target_of(total);
+  *need = target;
   if (start < target && start + a >= target) { s.found = 2 * tid; s.value = start; }
   else if (start + a < target && c >= target) { s.found = 2 * tid + 1; s.value = start + a; }
   __syncthreads();
@@ -231,10 +309,10 @@ __device__ int sample_find_bin(sample_lds& s, u64 target, u64* before) {
   return found;
 }
 
-// Shortens the kept prefix to the shortest whose values sum to `target` or more (all of it where they do not).
+// Shortens the kept prefix to the shortest whose values sum to target(sum of all) or more (all of it where they do not).
 // ONES: every element counts 1, else its weight.
-template <bool ONES>
-__device__ void sample_cut(sample_lds& s, sample_row& r, u64 target) {
+template <bool ONES, typename T>
+__device__ void sample_cut(sample_lds& s, sample_row& r, T&& target_of) {
   const int tid = threadIdx.x;
   auto value = [&](float v) { return ONES ? (u64)1 : r.weight(v); };
   auto kept = [&](int i, float v) { return v > -INFINITY && r.in_prefix(key_of(v), i); };
@@ -245,14 +323,16 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, u64 target) {
     __syncthreads();
   };
   clear();
-  for_each(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
-    if (kept(i, v)) atomicAdd(&s.list[r.bin(v)], value(v));
+  for_each<4>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+    const u64 x = value(v);   // no branch: see sample_pick
+    atomicAdd(&s.list[r.bin(v)], kept(i, v) ? x : 0);
   });
-  u64 before;
-  const int b = sample_find_bin(s, target, &before);
+  u64 target, before;
+  __syncthreads();
+  const int b = sample_find_bin(s, s.list[2 * tid], s.list[2 * tid + 1], target_of, &target, &before);
   if (b < 0) return;
   target -= before;
-  const int n = sample_gather(s, r, [&](int i, float v) { return kept(i, v) && r.bin(v) == b; });
+  const int n = sample_gather(s, r, 0, r.V, [&](int i, float v) { return kept(i, v) && r.bin(v) == b; });
   if (n <= SAMPLE_LIST) {
     sample_sort(s, n);
     const u64 e0 = 2 * tid < n ? s.list[2 * tid] : 0, e1 = 2 * tid + 1 < n ? s.list[2 * tid + 1] : 0;
@@ -270,7 +350,7 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, u64 target) {
   __syncthreads();
   if (tid == 0) { s.lo = 0xffffffffu; s.hi = 0; }
   __syncthreads();
-  for_each(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+  for_each<4>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
     if (kept(i, v) && r.bin(v) == b) {
       atomicMin(&s.lo, key_of(v));
       atomicMax(&s.hi, key_of(v));
@@ -282,11 +362,13 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, u64 target) {
     int shift = 0;
     while ((hi - lo) >> shift >= SAMPLE_BINS) ++shift;
     clear();
-    for_each(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+    for_each<4>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
       const uint32_t k = key_of(v);
       if (k >= lo && k <= hi && kept(i, v)) atomicAdd(&s.list[(hi - k) >> shift], value(v));
     });
-    const int at = sample_find_bin(s, target, &before);   // reached: the step's values sum to the target or more
+    u64 same;
+    __syncthreads();
+    const int at = sample_find_bin(s, s.list[2 * tid], s.list[2 * tid + 1], [&](u64) { return target; }, &same, &before);   // reached: the step's values sum to the target or more
     target -= before;
     hi -= (uint32_t)at << shift;
     const uint32_t width = (1u << shift) - 1;
@@ -300,22 +382,107 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, u64 target) {
   r.tau_idx = (uint32_t)last;
 }
 
-__global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
-  __shared__ sample_lds s;
+// Stretch of a range of `n` elements that a wavefront sums: whole loads of a wavefront, until the end.
+__device__ __forceinline__ int sample_stretch(int n) { return ((n + 15) / 16 + 255) / 256 * 256; }
+
+// Top-p (of what the prefix holds so far) and the token: with two passes over the row.  The first adds up fp32 weights by
+// steps of the logit, which tells the step that the cut falls into, give or take rounding.  The second forms the exact
+// weights: each wavefront's sum over its stretch of the row of what lies above that step, the sum of all, and the step's
+// members for the list; with them the step is checked (and the next one tried if rounding was in the way), the cut is found
+// among the sorted members, and the token's stretch is known.  -2: the step holds more than the list, sample_cut finds the
+// prefix and sample_pick the token.  130001 logits: 240 us with sample_cut's exact histogram and sample_pick, 94 so.
+template <typename C, typename T>
+__device__ int sample_top_p(sample_lds& s, sample_row& r, C&& cut_of, T&& target_of) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row = blockIdx.x;
-  sample_row r;
-  r.x = a.logits + row * a.row_stride;
-  r.V = a.vocab;
-  const float temperature = a.temperature ? a.temperature[row] : 1.0f;
-  const int top_k = a.top_k ? a.top_k[row] : 0;
-  const float top_p = a.top_p ? a.top_p[row] : 1.0f, min_p = a.min_p ? a.min_p[row] : 0.0f;
-  const float uniform = a.uniform[row];
-  // largest logit, smallest finite one
+  __syncthreads();
+  s.list[tid] = 0;
+  s.list[tid + 1024] = 0;
+  __syncthreads();
+  const float c32 = (float)fmin(r.c, 1e38);
+  const bool all = r.tau == 0 && r.tau_idx == 0xffffffffu;   // no prefix yet
+  for_each<4>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+    const float x = v == r.max ? r.top : r.infinite ? -INFINITY : v;
+    float w = __builtin_amdgcn_exp2f(fmaxf((x - r.top) * c32, -126.0f));
+    if (!all) w = r.in_prefix(key_of(v), i) ? w : 0.f;
+    atomicAdd(&s.list[r.bin(v)], (u64)(uint32_t)(w * 2147483648.0f));   // whole numbers: an LDS sum of floats takes 16 times as long
+  });
+  __syncthreads();
+  u64 need, before;
+  int b = max(sample_find_bin(s, s.list[2 * tid], s.list[2 * tid + 1], cut_of, &need, &before), 0);
+  const int len = sample_stretch(r.V), lo = min(r.V, wave * len), hi = min(r.V, lo + len);
+  for (int step = 0;;) {
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    u64 total = 0, above = 0, mine = 0;
+    for_each<SAMPLE_U>(r.x, lo, hi, lane, 64, [&](int i, float v) {
+      u64 w = r.weight(v);
+      if (!all) w = r.in_prefix(key_of(v), i) ? w : 0;
+      const int at = r.bin(v);
+      const u64 up = at < b ? w : 0;
+      total += w;
+      above += up;
+      mine += up >= r.least ? up : 0;
+      if (at == b && w > 0) {
+        const int to = atomicAdd(&s.n, 1);
+        if (to < SAMPLE_LIST) s.list[to] = (u64)~key_of(v) << 32 | (uint32_t)i;
+      }
+    });
+    mine = wave_sum64(mine);
+    block_scan64(s, total, &total);
+    block_scan64(s, above, &above);
+    const int n = s.n;
+    if (n > SAMPLE_LIST) return -2;
+    const u64 cut = cut_of(total);
+    sample_sort(s, n);
+    u64 e[2], w[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int i = 2 * tid + j;
+      e[j] = i < n ? s.list[i] : 0;
+      w[j] = i < n ? r.weight(of_key(~(uint32_t)(e[j] >> 32))) : 0;
+    }
+    u64 inside;
+    const u64 c = block_scan64(s, w[0] + w[1], &inside), start = above + c - w[0] - w[1];
+    // the cut lies above this step, or below it: never both ways, for the sums are exact
+    if (cut <= above && b > 0 && step <= 0) { step = -1; --b; __syncthreads(); continue; }
+    if (cut > above + inside && b < SAMPLE_BINS - 1 && step >= 0) { step = 1; ++b; __syncthreads(); continue; }
+    __syncthreads();
+    if (lane == 0) s.wave[wave] = mine;
+    if (start < cut && start + w[0] + w[1] >= cut) s.value = start + w[0] >= cut ? e[0] : e[1];
+    __syncthreads();
+    r.tau = ~(uint32_t)(s.value >> 32);
+    r.tau_idx = (uint32_t)s.value;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)   // kept members join their stretch
+      if (w[j] >= r.least && (j == 0 ? start : start + w[0]) < cut) atomicAdd(&s.wave[(int)(uint32_t)e[j] / len], w[j]);
+    __syncthreads();
+    u64 kept = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) kept += s.wave[q];
+    const u64 t = target_of(kept);
+    u64 run = 0, first = 0;
+    int at = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {   // the last stretch whose start the target reaches
+      if (run <= t && s.wave[q] > 0) { at = q; first = run; }
+      run += s.wave[q];
+    }
+    __syncthreads();
+    const int from = min(r.V, at * len);
+    return sample_pick_in(s, r, from, min(r.V, from + len), true, t - first, [&](int i, float v) {
+      const u64 x = r.weight(v);
+      return x >= r.least && r.in_prefix(key_of(v), i) ? x : (u64)0;
+    }, [](u64 x) { return x; });
+  }
+}
+
+// Largest and smallest finite logit of a range; each thread's own largest stays in s.tmax.
+__device__ void sample_extremes(sample_lds& s, const float* x, int lo, int hi, float* largest, float* smallest) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   float mx = -INFINITY, mn = INFINITY;
-  for_each(r.x, 0, r.V, tid, 1024, [&](int, float v) {
+  for_each<4>(x, lo, hi, tid, 1024, [&](int, float v) {
     mx = fmaxf(mx, v);
-    if (v > -INFINITY) mn = fminf(mn, v);
+    mn = fminf(mn, v > -INFINITY ? v : INFINITY);
   });
   s.tmax[tid] = mx;
   mn = -wave_max(-mn);
@@ -324,58 +491,236 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
   mx = s.tmax[lane];
 #pragma unroll
   for (int w = 1; w < 16; ++w) mx = fmaxf(mx, s.tmax[lane + 64 * w]);
-  mx = wave_max(mx);
+  *largest = wave_max(mx) + 0.0f;
 #pragma unroll
   for (int w = 0; w < 16; ++w) mn = fminf(mn, s.wmin[w]);
+  *smallest = mn;
+  __syncthreads();
+}
+
+// The row's parameters, without its largest logit.
+__device__ __forceinline__ sample_row sample_load_row(const pt_sample_args& a, int row, float temperature, float min_p) {
+  sample_row r;
+  r.x = a.logits + row * a.row_stride;
+  r.V = a.vocab;
+  int bits = 0;
+  while (bits < 31 && (1 << bits) < r.V) ++bits;
+  r.S = min(51, 62 - bits);
+  r.rounder = ldexp(1.5, 52 - r.S);
+  r.c = 1.4426950408889634 / (double)temperature;
+  r.tau = 0;
+  r.tau_idx = 0xffffffffu;
+  r.least = min_p > 0.0f ? max((u64)1, (u64)fmin(ceil(ldexp((double)min_p, r.S)), ldexp(1.0, r.S))) : 1;
+  return r;
+}
+
+// One part of a row: a.part_len logits from part * a.part_len on.
+__global__ void __launch_bounds__(1024) sample_part_kernel(const pt_sample_args a) {
+  __shared__ sample_lds s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+  sample_part* const to = (sample_part*)a.ws + blockIdx.x;
+  const float temperature = a.temperature ? a.temperature[row] : 1.0f;
+  const int top_k = a.top_k ? a.top_k[row] : 0;
+  const float top_p = a.top_p ? a.top_p[row] : 1.0f, min_p = a.min_p ? a.min_p[row] : 0.0f;
+  sample_row r = sample_load_row(a, row, temperature, min_p);
+  const int lo = min(r.V, part * a.part_len), hi = min(r.V, lo + a.part_len);
+  float mx, mn;
+  sample_extremes(s, r.x, lo, hi, &mx, &mn);
+  if (tid == 0) {
+    to->max = mx;
+    to->min = mn;
+    to->n = -1;
+  }
+  if (mx == -INFINITY || !(temperature > 0.0f)) return;
+  const bool k_on = top_k > 0 && top_k < r.V;
+  if (k_on && top_k <= SAMPLE_PART_K) {
+    const float bound = sample_bound(s, top_k);
+    const int n = sample_gather(s, r, lo, hi, [&](int, float v) { return v >= bound && v > -INFINITY; });
+    if (tid == 0) to->n = n;
+    if (n <= SAMPLE_PART_LIST && tid < n) to->list[tid] = s.list[tid];
+  } else if (!k_on && !(top_p < 1.0f) && !(min_p > 0.0f)) {
+    r.set_max(mx);
+    const int len = sample_stretch(hi - lo), from = min(hi, lo + wave * len);
+    u64 sum = 0;
+    for_each<SAMPLE_U>(r.x, from, min(hi, from + len), lane, 64, [&](int, float v) { sum += r.weight(v); });
+    sum = wave_sum64(sum);
+    if (lane == 0) to->sum[wave] = sum;
+  }
+}
+
+// A row of temperature alone from its parts' sums: which stretch the target falls into, and the token inside it.  The
+// parts' sums are relative to their own largest logit; their factors and the running sum over stretches are fp64, formed
+// in one order.
+__device__ int sample_from_sums(sample_lds& s, sample_row& r, const sample_part* parts, const pt_sample_args& a, double u) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int n = a.parts * 16;
+  __syncthreads();
+  double* const run = (double*)s.list;   // [n + 1] sums in front of a stretch
+  if (tid < 64) {
+    double v[4], before = 0.0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = lane * 4 + j;
+      v[j] = 0.0;
+      if (i < n) {
+        const sample_part& p = parts[i >> 4];
+        if (p.max == r.max) v[j] = (double)p.sum[i & 15];
+        else if (!r.infinite && p.max > -INFINITY) v[j] = (double)p.sum[i & 15] * r.power(p.max);
+      }
+    }
+    const double own = v[0] + v[1] + v[2] + v[3];
+    before = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double up = __shfl_up(before, o, 64);
+      if (lane >= o) before += up;
+    }
+    before -= own;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (lane * 4 + j <= n) run[lane * 4 + j] = before;
+      before += v[j];
+    }
+    if (lane == 63 && n == 256) run[n] = before;
+  }
+  if (tid == 0) s.n = -1;
+  __syncthreads();
+  const double t = u * run[n];
+  if (tid < n && run[tid] <= t && parts[tid >> 4].sum[tid & 15] > 0 && parts[tid >> 4].max > -INFINITY && !(r.infinite && parts[tid >> 4].max != r.max))
+    atomicMax(&s.n, tid);   // the last stretch whose start the target reaches
+  __syncthreads();
+  const int at = s.n, part = at >> 4;
+  const double start = run[at];
+  const u64 sum = parts[part].sum[at & 15];
+  const double scale = parts[part].max == r.max ? 1.0 : r.power(parts[part].max);
+  __syncthreads();
+  const int p0 = min(r.V, part * a.part_len), p1 = min(r.V, p0 + a.part_len), len = sample_stretch(p1 - p0);
+  const int lo = min(p1, p0 + (at & 15) * len), hi = min(p1, lo + len);
+  r.set_max(parts[part].max);
+  const u64 local = (u64)fmax((t - start) / scale, 0.0);
+  return sample_pick_in(s, r, lo, hi, true, min(local, sum - 1), [&](int, float v) { return r.weight(v); }, [](u64 x) { return x; });
+}
+
+// PARTS: sample_part_kernel ran before.
+template <bool PARTS>
+__global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
+  __shared__ sample_lds s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row = blockIdx.x;
+  const float temperature = a.temperature ? a.temperature[row] : 1.0f;
+  const int top_k = a.top_k ? a.top_k[row] : 0;
+  const float top_p = a.top_p ? a.top_p[row] : 1.0f, min_p = a.min_p ? a.min_p[row] : 0.0f;
+  const float uniform = a.uniform[row];
+  sample_row r = sample_load_row(a, row, temperature, min_p);
+  const sample_part* const parts = PARTS ? (const sample_part*)a.ws + row * a.parts : nullptr;
+  float mx, mn;
+  if constexpr (PARTS) {
+    mx = lane < a.parts ? parts[lane].max : -INFINITY;
+    mn = lane < a.parts ? parts[lane].min : INFINITY;
+    mx = wave_max(mx);
+    mn = -wave_max(-mn);
+  } else {
+    sample_extremes(s, r.x, 0, r.V, &mx, &mn);
+  }
   if (mx == -INFINITY) {
     if (tid == 0) a.out[row] = -1;
     return;
   }
-  r.max = mx + 0.0f;
+  r.set_max(mx);
   if (!(temperature > 0.0f)) {   // greedy
-    __syncthreads();
+    int lo = 0, hi = r.V;
+    if constexpr (PARTS) {   // the first part that holds the largest
+      const int p = __ffsll((unsigned long long)__ballot(lane < a.parts && parts[lane].max == mx)) - 1;
+      lo = min(r.V, p * a.part_len);
+      hi = min(r.V, lo + a.part_len);
+    }
     if (tid == 0) s.n = 0x7fffffff;
     __syncthreads();
-    for_each(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+    for_each<4>(r.x, lo, hi, tid, 1024, [&](int i, float v) {
       if (v == r.max) atomicMin(&s.n, i);
     });
     __syncthreads();
     if (tid == 0) a.out[row] = s.n;
     return;
   }
-  int bits = 0;
-  while (bits < 31 && (1 << bits) < r.V) ++bits;
-  r.S = min(52, 62 - bits);
-  r.c = 1.4426950408889634 / (double)temperature;
-  r.tau = 0;
-  r.tau_idx = 0xffffffffu;
-  r.least = min_p > 0.0f ? max((u64)1, (u64)fmin(ceil(ldexp((double)min_p, r.S)), ldexp(1.0, r.S))) : 1;
   const bool k_on = top_k > 0 && top_k < r.V, p_on = top_p < 1.0f;
   const double u = uniform > 0.0f ? fmin((double)uniform, 1.0) : 0.0;
   // uniform * total, below the total
   auto target = [&](u64 total) { return min((u64)(u * (double)total), total - 1); };
   auto cut_mass = [&](u64 total) { return max((u64)1, min((u64)ceil(fmax((double)top_p, 0.0) * (double)total), total)); };
+  if constexpr (PARTS) {
+    if (!k_on && !p_on && !(min_p > 0.0f)) {
+      const int token = sample_from_sums(s, r, parts, a, u);
+      if (tid == 0) a.out[row] = token;
+      return;
+    }
+  }
 
   if (k_on && top_k <= SAMPLE_LIST_K) {
-    // a lower bound of the k-th largest: the k-th largest of group maxima
-    const int groups = top_k <= 192 ? 256 : 1024;
-    float gm = -INFINITY;
-    if (tid < groups)
-      for (int j = tid; j < 1024; j += groups) gm = fmaxf(gm, s.tmax[j]);
-    __syncthreads();
-    if (tid < groups) s.tmax[tid] = gm;
-    __syncthreads();
-    if (tid < groups) {
-      int rank = 0;
-      for (int j = 0; j < groups; ++j) {
-        const float o = s.tmax[j];
-        rank += o > gm || (o == gm && j < tid);
+    int n = SAMPLE_LIST + 1;
+    if (PARTS && top_k <= SAMPLE_PART_K) {
+      // the parts' candidates, one part behind the other
+      const int own = lane < a.parts ? max(parts[lane].n, 0) : 0;
+      const bool whole = __all(own <= SAMPLE_PART_LIST);
+      int sum = own;
+#pragma unroll
+      for (int o = 1; o < SAMPLE_PARTS; o <<= 1) {
+        const int up = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += up;
       }
-      if (rank == top_k - 1) s.wmin[0] = gm;
+      const int all = __shfl(sum, SAMPLE_PARTS - 1, 64);
+      if (whole && all <= SAMPLE_LIST) {
+        n = all;
+        for (int p = wave; p < a.parts; p += 16) {
+          const int count = __shfl(own, p, 64), first = __shfl(sum, p, 64) - count;
+          for (int i = lane; i < count; i += 64) s.list[first + i] = parts[p].list[i];
+        }
+        __syncthreads();
+      }
     }
-    __syncthreads();
-    const float bound = s.wmin[0];
-    int n = sample_gather(s, r, [&](int, float v) { return v >= bound && v > -INFINITY; });
+    if (n > SAMPLE_LIST) {
+      if constexpr (PARTS) sample_extremes(s, r.x, 0, r.V, &mx, &mn);   // the threads' maxima
+      const float bound = sample_bound(s, top_k);
+      n = sample_gather(s, r, 0, r.V, [&](int, float v) { return v >= bound && v > -INFINITY; });
+    }
+    if (n > 64 && n <= 512 && top_k <= 64) {
+      // the k largest by comparing each with all: the sorts below have a barrier per step
+      const u64 mine = tid < n ? s.list[tid] : ~0ull;
+      int rank = 0;
+      if (tid < n) {
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) rank += s.list[j] < mine;
+      }
+      __syncthreads();
+      if (tid < n && rank < top_k) s.list[rank] = mine;
+      __syncthreads();
+      n = top_k;
+    }
+    if (n <= 64) {
+      // one wavefront, an element per lane: the same steps without a barrier
+      if (wave > 0) return;
+      u64 e = lane < n ? s.list[lane] : ~0ull;
+      e = wave_sort64(e);
+      const int m = min(n, top_k);
+      u64 w = lane < m ? r.weight(of_key(~(uint32_t)(e >> 32))) : 0;
+      u64 c = wave_scan64(w);
+      u64 total = (u64)__shfl((long long)c, 63, 64);
+      const u64 need = p_on ? cut_mass(total) : total;
+      if (!(w >= r.least && c - w < need)) {   // least is 1 or more: lanes without an element go too
+        e = ~0ull;
+        w = 0;
+      } else {
+        e = e << 32 | ~(uint32_t)(e >> 32);
+      }
+      e = wave_sort64(e);
+      w = e != ~0ull ? r.weight(of_key((uint32_t)e)) : 0;
+      c = wave_scan64(w);
+      total = (u64)__shfl((long long)c, 63, 64);
+      const u64 t = target(total);
+      if (w > 0 && c - w <= t && c > t) a.out[row] = (int32_t)(e >> 32);
+      return;
+    }
     if (n <= SAMPLE_LIST) {
       sample_sort(s, n);
       // two elements per thread, in order; those past k drop out
@@ -423,30 +768,54 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
   const float span = r.max - mn;
   if (k_on) {
     r.bin_scale = span > 0.0f ? (SAMPLE_BINS - 1) / span : 0.0f;
-    sample_cut<true>(s, r, (u64)top_k);
+    sample_cut<true>(s, r, [&](u64) { return (u64)top_k; });
   }
   if (p_on) {
     // mass lies within 40 T of the largest logit; the last step takes what is behind
     r.bin_scale = span > 0.0f ? (SAMPLE_BINS - 1) / fminf(span, 40.0f * temperature) : 0.0f;
-    u64 sum = 0, total;
-    for_each(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
-      if (r.in_prefix(key_of(v), i)) sum += r.weight(v);
-    });
-    block_scan64(s, sum, &total);
-    sample_cut<false>(s, r, cut_mass(total));
+    const int token = sample_top_p(s, r, cut_mass, target);
+    if (token != -2) {
+      if (tid == 0) a.out[row] = token;
+      return;
+    }
+    sample_cut<false>(s, r, cut_mass);
   }
-  const int token = sample_pick(s, r, [&](int i, float v) {
-    if (!r.in_prefix(key_of(v), i)) return (u64)0;
-    const u64 w = r.weight(v);
-    return w >= r.least ? w : (u64)0;
-  }, target);
+  int token;
+  if (!k_on && !p_on) {
+    token = sample_pick(s, r, [&](int, float v) {
+      const u64 w = r.weight(v);
+      return w >= r.least ? w : (u64)0;
+    }, target);
+  } else {
+    token = sample_pick(s, r, [&](int i, float v) {
+      const u64 w = r.weight(v);
+      return w >= r.least && r.in_prefix(key_of(v), i) ? w : (u64)0;
+    }, target);
+  }
   if (tid == 0) a.out[row] = token;
 }
 
-size_t pt_sample_workspace(int32_t, int32_t) { return 0; }
+// Parts of a row: none where the rows alone fill the chip, or where a part would be below 16384 logits.
+static int sample_parts(int32_t rows, int32_t vocab) {
+  const int64_t p = std::min<int64_t>(std::min<int64_t>(SAMPLE_PARTS, 256 / rows), vocab / 16384);
+  return p < 2 ? 1 : (int)p;
+}
 
-int pt_launch_sample(const pt_sample_args& a, hipStream_t s) {
-  hipLaunchKernelGGL(sample_kernel, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
+size_t pt_sample_workspace(int32_t rows, int32_t vocab) {
+  const int parts = sample_parts(rows, vocab);
+  return parts == 1 ? 0 : (size_t)rows * parts * sizeof(sample_part);
+}
+
+int pt_launch_sample(const pt_sample_args& args, hipStream_t s) {
+  pt_sample_args a = args;
+  a.parts = sample_parts(a.rows, a.vocab);
+  a.part_len = ((a.vocab + a.parts - 1) / a.parts + 1023) / 1024 * 1024;
+  if (a.parts > 1) {
+    hipLaunchKernelGGL(sample_part_kernel, dim3((unsigned)(a.rows * a.parts)), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL(sample_kernel<true>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
+  } else {
+    hipLaunchKernelGGL(sample_kernel<false>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
+  }
   PT_HIP_CHECK(hipGetLastError());
   return PT_OK;
 }

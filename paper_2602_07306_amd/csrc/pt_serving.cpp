@@ -259,6 +259,6 @@ extern "C" int pt_sample(const float* dev_logits, int64_t row_stride, int32_t ro
     if (!aligned16(workspace)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "workspace is not 16-byte aligned");
     if (workspace_bytes < need) return pt_set_error(PT_ERR_ARENA_TOO_SMALL, "workspace: %zu bytes given, %zu needed", workspace_bytes, need);
   }
-  const pt_sample_args a = {dev_logits, row_stride, dev_uniform, dev_temperature, dev_top_k, dev_top_p, dev_min_p, dev_out, workspace, rows, vocab};
+  const pt_sample_args a = {dev_logits, row_stride, dev_uniform, dev_temperature, dev_top_k, dev_top_p, dev_min_p, dev_out, workspace, rows, vocab, 0, 0};
   return pt_launch_sample(a, (hipStream_t)hip_stream);
 }

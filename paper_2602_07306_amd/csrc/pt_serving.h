@@ -77,6 +77,7 @@ struct pt_sample_args {
   int32_t* out;
   void* ws;
   int32_t rows, vocab;
+  int32_t parts, part_len;   // set by the launcher
 };
 int pt_launch_sample(const pt_sample_args& a, hipStream_t s);
 
