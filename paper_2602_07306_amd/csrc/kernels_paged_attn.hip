@@ -203,11 +203,9 @@ __device__ __forceinline__ void paged_merge(const pt_paged_attn_args& a, const p
 // ------------------------------------------------------------------------------------------------
 template <int HD>
 struct paged_geom {
-  static constexpr int TK = HD == 256 ? 32 : 64;      // keys of a tile
   static constexpr int ROWB = HD * 2, CH = HD / 8;    // bytes and 16-byte chunks of a row
   static constexpr int RPI = 64 / CH;                 // rows per load instruction of 1024 bytes
   static constexpr int PER16 = 16 / RPI;              // load instructions per 16 keys
-  static constexpr int TILE_B = TK * ROWB;
   // XOR of a row's chunk numbers.  A 16-byte read of 16 rows at once must meet 16 different chunks (of 256 bytes), a
   // transposing read of 8 rows at once 8 different pairs of chunks: the row's low bits choose the pair, a higher one the half.
   static __device__ __forceinline__ int swz(int row) { return HD == 64 ? (row & 6) | (row >> 3 & 1) : (row & 7) << 1 | (row >> 3 & 1); }
@@ -239,17 +237,17 @@ __device__ __forceinline__ void load_keys_to_lds(uint32_t lds, const char* base,
   }
 }
 
-template <int HD, int NQ, bool FULL>
-__global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_args a) {
+// TK: keys of a tile.
+template <int HD, int NQ, bool FULL, int TK>
+__device__ __forceinline__ void paged_few_rows(const pt_paged_attn_args& a, int block, char* smem) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using geo = paged_geom<HD>;
-  constexpr int TK = geo::TK, CH = geo::CH, RPI = geo::RPI, PER16 = geo::PER16, TILE_B = geo::TILE_B;
+  constexpr int CH = geo::CH, RPI = geo::RPI, PER16 = geo::PER16, TILE_B = TK * geo::ROWB;
   constexpr int NB = TK / 16, KS = HD / 32, HB = HD / 16, NU = TK / 32;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int kvh = blockIdx.x % a.Hkv;
-  const int rest = blockIdx.x / a.Hkv;
+  const int kvh = block % a.Hkv;
+  const int rest = block / a.Hkv;
   const int split = rest / a.cut[0].tiles;
   paged_tile t;
   if (!paged_find_tile<false>(a, rest - split * a.cut[0].tiles, &t) || split >= t.nsplit) return;
@@ -457,22 +455,27 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
 #endif
 }
 
+template <int HD, int NQ, bool FULL>
+__global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  paged_few_rows<HD, NQ, FULL, HD == 256 ? 32 : 64>(a, blockIdx.x, smem);
+}
+
 // ------------------------------------------------------------------------------------------------
 // bf16, many rows: four wavefronts of 32 packed rows each share key tiles of 64 (K and V as they lie in their pages, two
 // tiles in LDS: one that is read, one on its way).  A wavefront loads the tile's 16 keys of its number - one page - and
 // multiplies all 64 with its own rows; MFMA layouts, swizzle and transposing reads as above.
 // ------------------------------------------------------------------------------------------------
 template <int HD, bool FULL>
-__global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_attn_args a) {
+__device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int block, char* smem) {   // smem: [2][K tile], [2][V tile]
 #if defined(__HIP_DEVICE_COMPILE__)
   using geo = paged_geom<HD>;
   constexpr int TK = 64, CH = geo::CH, RPI = geo::RPI, PER16 = geo::PER16, ROWB = geo::ROWB, TILE_B = TK * ROWB;
   constexpr int NB = TK / 16, KS = HD / 32, HB = HD / 16, NU = TK / 32, NQ = 2;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];   // [2][K tile], [2][V tile]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int kvh = blockIdx.x % a.Hkv;
-  const int rest = blockIdx.x / a.Hkv;
+  const int kvh = block % a.Hkv;
+  const int rest = block / a.Hkv;
   const int split = rest / a.cut[1].tiles;
   paged_tile t;
   // the last tiles of a sequence see most: they come first
@@ -804,6 +807,31 @@ __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_
 #endif
 }
 
+template <int HD, bool FULL>
+__global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_attn_args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  paged_many_rows<HD, FULL>(a, blockIdx.x, smem);
+}
+
+// Decode steps beside chunks in one launch: workgroups of the one kind wait for HBM while those of the other multiply.  Stretches
+// of 64 workgroups are dealt to the two kinds in proportion (multiples of the 8 XCDs, so that a KV head stays on its own).
+// Two workgroups share a compute unit: the few rows' tiles hold half the keys at hd = 128.
+constexpr int PA_DEAL = 64;
+template <int HD, bool FULL>
+__global__ void __launch_bounds__(256, 2) paged_attn_both_kernel(const pt_paged_attn_args a, int many, int few) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int64_t all = many + few;                     // stretches
+  const int st = blockIdx.x / PA_DEAL, in = blockIdx.x % PA_DEAL;
+  const int before = (int)(st * (int64_t)many / all);   // stretches of the many-row kind in front of this one
+  if ((int)((st + 1) * (int64_t)many / all) > before) {
+    const int block = before * PA_DEAL + in;
+    if (block < a.cut[1].tiles * a.Hkv * a.cut[1].n_splits) paged_many_rows<HD, FULL>(a, block, smem);
+  } else {
+    const int block = (st - before) * PA_DEAL + in;
+    if (block < a.cut[0].tiles * a.Hkv * a.cut[0].n_splits) paged_few_rows<HD, 1, FULL, HD == 128 ? 32 : 64>(a, block, smem);
+  }
+}
+
 // ------------------------------------------------------------------------------------------------
 // fp32, on 16x16x4 MFMAs: 16 packed rows per workgroup, 16 keys per wavefront and step, operands straight from the pages.
 // The contraction over the head takes elements 16 j + 4 g + i in step (j, i), so that a lane's operands are 16-byte loads; the
@@ -986,7 +1014,7 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
   // enough ranges for 2048 workgroups, each of at least a tile for every wavefront
   if (t0 > 0) paged_ranges(t0 * Hkv, keys, 2048, 256, &p->cut[0]);
   if (t1 > 0) paged_ranges(t1 * Hkv, keys, 512, 256, &p->cut[1]);
-  if (t0 * Hkv * std::max(2, p->cut[0].n_splits) > 0x7fffffff || t1 * Hkv * std::max(8, p->cut[1].n_splits) > 0x7fffffff)
+  if (t0 * Hkv * std::max(2, p->cut[0].n_splits) > 0x3fffffff || t1 * Hkv * std::max(8, p->cut[1].n_splits) > 0x3fffffff)
     return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
   const int32_t splits = std::max(p->cut[0].n_splits, p->cut[1].n_splits);
   if (splits > 1) {
@@ -999,7 +1027,7 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
 
 template <int HD, int NQ, bool FULL>
 static int launch_paged(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
-  constexpr int LDS = std::max(8 * paged_geom<HD>::TILE_B, 4 * 16 * NQ * ((HD + 4) * 4 + 8));
+  constexpr int LDS = std::max(8 * (HD == 256 ? 32 : 64) * paged_geom<HD>::ROWB, 4 * 16 * NQ * ((HD + 4) * 4 + 8));
   static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
   auto kern = paged_attn_kernel<HD, NQ, FULL>;
   PT_SET_MAX_LDS_ONCE(kern, LDS);
@@ -1031,14 +1059,31 @@ static void launch_combine(const pt_paged_attn_args& a, hipStream_t s) {
   hipLaunchKernelGGL((paged_combine_kernel<T, WIDE>), dim3(blocks), dim3(256), 0, s, a);
 }
 
+template <int HD, bool FULL>
+static int launch_both(const pt_paged_attn_args& a, hipStream_t s) {
+  constexpr int LDS = 64 * 1024;   // 4 tiles of 64 keys, or 8 of the few rows' own: the same at both widths or less
+  static_assert(LDS >= 4 * 64 * paged_geom<HD>::ROWB && LDS >= 8 * (HD == 128 ? 32 : 64) * paged_geom<HD>::ROWB && LDS >= 4 * 16 * ((HD + 4) * 4 + 8), "both kinds fit");
+  const int many = (int)(((int64_t)a.cut[1].tiles * a.Hkv * a.cut[1].n_splits + PA_DEAL - 1) / PA_DEAL);
+  const int few = (int)(((int64_t)a.cut[0].tiles * a.Hkv * a.cut[0].n_splits + PA_DEAL - 1) / PA_DEAL);
+  auto kern = paged_attn_both_kernel<HD, FULL>;
+  PT_SET_MAX_LDS_ONCE(kern, LDS);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(many + few) * PA_DEAL), dim3(256), LDS, s, a, many, few);
+  return PT_OK;
+}
+
 int pt_launch_paged_attn(const pt_paged_attn_args& a, int32_t dtype, hipStream_t s) {
   int rc = PT_OK;
-  if (a.cut[1].tiles > 0) {
+  const bool both = a.cut[0].tiles > 0 && a.cut[1].tiles > 0 && a.cut[0].tile_rows == 16;
+  if (both) {
+    if (a.hd <= 64) rc = a.hd == 64 ? launch_both<64, true>(a, s) : launch_both<64, false>(a, s);
+    else rc = a.hd == 128 ? launch_both<128, true>(a, s) : launch_both<128, false>(a, s);
+  }
+  if (!both && a.cut[1].tiles > 0) {
     const unsigned grid = (unsigned)((int64_t)a.cut[1].tiles * a.Hkv * a.cut[1].n_splits);
     if (a.hd <= 64) rc = a.hd == 64 ? launch_wide<64, true>(a, grid, s) : launch_wide<64, false>(a, grid, s);
     else rc = a.hd == 128 ? launch_wide<128, true>(a, grid, s) : launch_wide<128, false>(a, grid, s);
   }
-  if (!rc && a.cut[0].tiles > 0) {
+  if (!rc && !both && a.cut[0].tiles > 0) {
     const unsigned grid = (unsigned)((int64_t)a.cut[0].tiles * a.Hkv * a.cut[0].n_splits);
     const int nq = a.cut[0].tile_rows / 16;
     if (dtype == PT_F32) {
