@@ -209,16 +209,23 @@ def _need(ok: bool, what: str) -> None:
         raise PTError(PT_ERR_INVALID_ARGUMENT, what)
 
 
+_current = None   # torch's (current stream of a device as a handle, current device, guard)
+
+
 def _launch(index: int, stream, fn, *args) -> None:
     """fn(*args, stream) on GPU `index`, on its current stream if none is given."""
-    import torch
+    global _current
     if index < 0:
         raise PTError(PT_ERR_INVALID_ARGUMENT, "the tensors must be on a GPU")
-    st = torch._C._cuda_getCurrentRawStream(index) if stream is None else getattr(stream, "cuda_stream", stream)
-    if torch._C._cuda_getDevice() == index:
+    if _current is None:
+        import torch
+        _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, torch.cuda.device
+    raw_stream, device, guard = _current
+    st = raw_stream(index) if stream is None else getattr(stream, "cuda_stream", stream)
+    if device() == index:
         rc = fn(*args, st)
     else:
-        with torch.cuda.device(index):
+        with guard(index):
             rc = fn(*args, st)
     if rc:
         _check(rc)

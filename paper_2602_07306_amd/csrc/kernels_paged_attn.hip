@@ -102,7 +102,8 @@ __device__ __forceinline__ bool paged_find_tile(const pt_paged_attn_args& a, int
 }
 
 // One row by one wavefront, keys k0 .. k1-1, touching no other key: lane = key for the scores, lane = element for the values.
-// For rows whose tile met an infinity or a NaN: a key that the mask drops still enters the tile's product, as 0 * V.
+// For rows whose result holds an infinity or a NaN while the keys behind them hold one among their values: a key that the
+// mask drops still enters the tile's product, as 0 * V.
 template <typename T>
 __device__ __forceinline__ void paged_row_alone(const pt_paged_attn_args& a, const T* q, const T* K, const T* V, const int32_t* pages, int k0, int k1,
                                              float* m_out, float* l_out, float acc[4]) {
@@ -140,6 +141,20 @@ __device__ __forceinline__ void paged_row_alone(const pt_paged_attn_args& a, con
   }
   *m_out = m;
   *l_out = l;
+}
+
+// Whether a value of the keys from .. to-1 is infinite or no number: lane = key.
+template <typename T>
+__device__ __forceinline__ bool paged_odd_values(const pt_paged_attn_args& a, const T* V, const int32_t* pages, int from, int to) {
+  bool odd = false;
+  for (int key = from + (int)(threadIdx.x & 63); key < to; key += 64) {
+    const T* v = V + paged_checked(a.b, pages[key >> a.b.page_shift]) * a.page_stride + (key & ((1 << a.b.page_shift) - 1)) * a.token_stride;
+    for (int e = 0; e < a.hd; e += 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd |= !(fabsf(elem<T>::ld(v + e + i)) < INFINITY);
+    }
+  }
+  return __any(odd);
 }
 
 // Result of one row over one range: the output itself, or a partial for the combine.
@@ -181,8 +196,8 @@ __device__ __forceinline__ void paged_merge(const pt_paged_attn_args& a, const p
       for (int w = 0; w < 4; ++w) o[j] += f[w] * red_o[(w * a.cut[0].tile_rows + r) * (HD + 4) + lane + 64 * j];
       if (lane + 64 * j < a.hd) odd |= !(fabsf(o[j]) < INFINITY);
     }
-    if (__any(odd)) {
-      const int64_t hoff = (int64_t)kvh * a.head_stride;
+    const int64_t hoff = (int64_t)kvh * a.head_stride;
+    if (__any(odd) && paged_odd_values<T>(a, (const T*)a.vc + hoff, a.b.pages + t.seq * a.b.pages_stride, max(k0, lim), k1)) {
       paged_row_alone<T>(a, (const T*)a.q + row * a.q_rs + head * a.q_hs, (const T*)a.kc + hoff, (const T*)a.vc + hoff,
                          a.b.pages + t.seq * a.b.pages_stride, k0, min(k1, lim), &m, &l, o);
     }
@@ -787,10 +802,14 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
         if (g == 0) a.part_ml[at] = make_float2(m, l);
       }
     }
-    // rows that met an infinity or a NaN: again, without the keys behind them
+    // rows that met an infinity or a NaN among the keys behind them: again, without those
     uint64_t again = __ballot(odd);
     again |= again >> 32;
     again |= again >> 16;
+    again &= 0xffff;
+    if (again && !paged_odd_values<bf16_t>(a, (const bf16_t*)a.vc + (int64_t)kvh * a.head_stride, a.b.pages + t.seq * a.b.pages_stride,
+                                           max(k0, lim_first), min(k1, k0 + own * UK + UK)))
+      again = 0;
     for (int j = 0; j < 16; ++j)
       if (again >> j & 1) {
         const int rj = t.row0 + w0 + n * 16 + j, ij = rj / G, hj = kvh * G + (rj - ij * G), rowj = t.sq.first + ij;
@@ -983,10 +1002,12 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(const pt_paged_attn_
 
 constexpr int PA_WIDE_ROWS = 128;
 
-// Ranges of keys for `units` workgroups: as many as it takes to have `want` of them, each of at least `least` keys.
-static void paged_ranges(int64_t units, int64_t keys, int64_t want, int64_t least, pt_paged_cut* c) {
-  int64_t splits = std::min<int64_t>((want + units - 1) / units, PA_MAX_SPLITS);
-  const int64_t chunk = ((keys + splits - 1) / splits + least - 1) / least * least;
+// Ranges of keys for `units` workgroups: as many as it takes to have `want` of them, each of at least 256 keys (a tile of 64 for
+// every wavefront).  One range where `single` keys are not exceeded: one sequence of 777 keys, 64 heads of 64, takes 8.5 us
+// in one and 5.4 + 3.9 in four with the launch that joins them.
+static void paged_ranges(int64_t units, int64_t keys, int64_t want, int64_t single, pt_paged_cut* c) {
+  int64_t splits = keys <= single ? 1 : std::min<int64_t>((want + units - 1) / units, PA_MAX_SPLITS);
+  const int64_t chunk = ((keys + splits - 1) / splits + 255) / 256 * 256;
   c->chunk = (int32_t)chunk;
   c->n_splits = (int32_t)((keys + chunk - 1) / chunk);
 }
@@ -1011,8 +1032,9 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
   }
   p->cut[0].tiles = (int32_t)std::min<int64_t>(t0, 0x7fffffff);
   p->cut[1].tiles = (int32_t)std::min<int64_t>(t1, 0x7fffffff);
-  // enough ranges for 2048 workgroups, each of at least a tile for every wavefront
-  if (t0 > 0) paged_ranges(t0 * Hkv, keys, 2048, 256, &p->cut[0]);
+  // Few rows: 2048 workgroups, so that sequences of different lengths even out (64 of 128 to 8192 keys on 16 KV heads: 387 us;
+  // 1024 workgroups, one range each, 383; 4096 395).  The fp32 kernel takes 64 keys at a time where the other takes 256.
+  if (t0 > 0) paged_ranges(t0 * Hkv, keys, 2048, dtype == PT_F32 ? 256 : 1024, &p->cut[0]);
   if (t1 > 0) paged_ranges(t1 * Hkv, keys, 512, 256, &p->cut[1]);
   if (t0 * Hkv * std::max(2, p->cut[0].n_splits) > 0x3fffffff || t1 * Hkv * std::max(8, p->cut[1].n_splits) > 0x3fffffff)
     return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");

@@ -136,6 +136,21 @@ def test_a_later_position_has_no_influence(dtype, hd, bad):
         assert not torch.isfinite(out[first + n - 1].float()).all()
 
 
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
+def test_a_visible_position_has_all_its_influence(dtype, hd):
+    """No number among the keys that every row sees: every row is none, and nothing is taken for a key behind it."""
+    lens = [(40, 140), (150, 400), (1, 30)]
+    p = Problem(4, 2, hd, dtype, 16, lens, seed=19)
+    for b in range(3):
+        p.v5[p.layer, p.table[b, 0], :, 3, 5] = float("inf")
+    out = p.run()
+    used = int(p.row_start[-1])
+    assert torch.all(out[:used, :, 5] == float("inf"))
+    keep = [c for c in range(hd) if c != 5]
+    p.v5[p.layer, p.table[[0, 1, 2], 0], :, 3, 5] = 0
+    assert torch.equal(out[:used][..., keep], p.run()[:used][..., keep])
+
+
 @pytest.mark.parametrize("H,Hkv,hd,dtype", [(2, 2, 128, "bf16"), (8, 1, 64, "bf16"), (2, 1, 64, "fp32")])
 def test_long_sequences_cut_into_ranges(H, Hkv, hd, dtype):
     p = Problem(H, Hkv, hd, dtype, 64, [(1, 5003), (1, 130), (3, 2049), (1, 1)], seed=8)
