@@ -312,9 +312,10 @@ int pt_page_copy(const pt_paged_cache* cache, const int32_t* host_pairs, int32_t
  *   out  = the first token, in order of index, at which the running sum of the kept weights exceeds uniform * their sum
  * Parameters are device arrays of `rows` entries: uniform fp32 in [0, 1) (values outside are taken as the nearer end);
  * temperature fp32 (0, negative or NaN: the largest logit, lowest index on ties), top_k int32, top_p fp32, min_p fp32, each of
- * which may be NULL (temperature 1; filter off).  Weights and sums are in 64 bits and formed in an order that does not
- * change, so equal inputs give equal tokens.  A row without any weight gives -1; where +infinity occurs, the tokens that have
- * it share the weight equally.
+ * which may be NULL (temperature 1; filter off).  Weights and sums are whole multiples of 2^-S of the largest weight, S = 51 up
+ * to 2048 tokens and one less for each doubling of vocab from there on (lighter tokens come only of uniform = 0), and formed so that equal
+ * inputs give equal tokens.  A row without any weight gives -1; where +infinity occurs, the tokens that have it share the
+ * weight equally.
  *   vocab      1..2^24
  *   workspace  16-byte aligned device memory of pt_sample_bytes, or NULL where that is 0; needs no clearing
  * Errors: NULL_POINTER, INVALID_ARGUMENT, ARENA_TOO_SMALL. */

@@ -782,7 +782,15 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
 #pragma unroll
       for (int v = 0; v < 4; ++v) odd |= !(fabsf(acc[n][hb][v]) < INFINITY);
     odd &= real;
-    if (real) {
+    // rows that met an infinity or a NaN among the keys behind them: again, without those
+    uint64_t again = __ballot(odd);
+    again |= again >> 32;
+    again |= again >> 16;
+    again &= 0xffff;
+    if (again && !paged_odd_values<bf16_t>(a, (const bf16_t*)a.vc + (int64_t)kvh * a.head_stride, a.b.pages + t.seq * a.b.pages_stride,
+                                           max(k0, lim_first), min(k1, k0 + own * UK + UK)))
+      again = 0;
+    if (real && !(again >> l16 & 1)) {   // the others' queries are read once more, and the output may lie over them
       const int64_t at = ((int64_t)split * a.b.total_rows + row) * a.H + head;
       if (t.nsplit == 1) {
         const float inv = see <= 0 ? 0.f : 1.0f / l;
@@ -802,14 +810,6 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
         if (g == 0) a.part_ml[at] = make_float2(m, l);
       }
     }
-    // rows that met an infinity or a NaN among the keys behind them: again, without those
-    uint64_t again = __ballot(odd);
-    again |= again >> 32;
-    again |= again >> 16;
-    again &= 0xffff;
-    if (again && !paged_odd_values<bf16_t>(a, (const bf16_t*)a.vc + (int64_t)kvh * a.head_stride, a.b.pages + t.seq * a.b.pages_stride,
-                                           max(k0, lim_first), min(k1, k0 + own * UK + UK)))
-      again = 0;
     for (int j = 0; j < 16; ++j)
       if (again >> j & 1) {
         const int rj = t.row0 + w0 + n * 16 + j, ij = rj / G, hj = kvh * G + (rj - ij * G), rowj = t.sq.first + ij;

@@ -67,6 +67,7 @@ struct sample_row {
   double c;                    // log2 e / T
   double rounder;              // 1.5 * 2^(52 - S)
   uint32_t tau, tau_idx;       // last element kept by top-k and top-p
+  float min_p;
   u64 least;                   // min-p as a weight
   float bin_scale;
 
@@ -91,6 +92,10 @@ struct sample_row {
     return __hiloint2double(__double2hiint(p) + (__double2loint(shifted) << 20), __double2loint(p));
   }
   __device__ __forceinline__ u64 weight(float v) const { return (u64)__double_as_longlong(power(v) + rounder) - (u64)__double_as_longlong(rounder); }
+  // any weight at all, and min-p's
+  __device__ __forceinline__ bool has_weight(float v) const {
+    return v == max || (!infinite && v > -INFINITY && ((double)v - (double)max) * c > -1074.0 && (!(min_p > 0.0f) || power(v) >= (double)min_p));
+  }
   __device__ __forceinline__ void set_max(float m) {
     max = m;
     infinite = m == INFINITY;
@@ -279,7 +284,7 @@ __device__ int sample_gather(sample_lds& s, const sample_row& r, int lo, int hi,
   __syncthreads();
   if (threadIdx.x == 0) s.n = 0;
   __syncthreads();
-  for_each<4>(r.x, lo, hi, threadIdx.x, 1024, [&](int i, float v) {
+  for_each<2>(r.x, lo, hi, threadIdx.x, 1024, [&](int i, float v) {
     if (take(i, v)) {
       const int at = atomicAdd(&s.n, 1);
       if (at < SAMPLE_LIST) s.list[at] = (u64)~key_of(v) << 32 | (uint32_t)i;
@@ -323,7 +328,7 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, T&& target_of) {
     __syncthreads();
   };
   clear();
-  for_each<4>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+  for_each<2>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
     const u64 x = value(v);   // no branch: see sample_pick
     atomicAdd(&s.list[r.bin(v)], kept(i, v) ? x : 0);
   });
@@ -350,7 +355,7 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, T&& target_of) {
   __syncthreads();
   if (tid == 0) { s.lo = 0xffffffffu; s.hi = 0; }
   __syncthreads();
-  for_each<4>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+  for_each<2>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
     if (kept(i, v) && r.bin(v) == b) {
       atomicMin(&s.lo, key_of(v));
       atomicMax(&s.hi, key_of(v));
@@ -362,7 +367,7 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, T&& target_of) {
     int shift = 0;
     while ((hi - lo) >> shift >= SAMPLE_BINS) ++shift;
     clear();
-    for_each<4>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+    for_each<2>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
       const uint32_t k = key_of(v);
       if (k >= lo && k <= hi && kept(i, v)) atomicAdd(&s.list[(hi - k) >> shift], value(v));
     });
@@ -382,6 +387,19 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, T&& target_of) {
   r.tau_idx = (uint32_t)last;
 }
 
+// The answer to a uniform number of 0: the first token of the prefix that has any weight, however small (down to 2^-1074, where
+// fp64 ends; as integers of 2^-S most of those are 0).
+__device__ int sample_first(sample_lds& s, const sample_row& r) {
+  __syncthreads();
+  if (threadIdx.x == 0) s.n = 0x7fffffff;
+  __syncthreads();
+  for_each<2>(r.x, 0, r.V, threadIdx.x, 1024, [&](int i, float v) {
+    if (r.has_weight(v) && r.in_prefix(key_of(v), i)) atomicMin(&s.n, i);
+  });
+  __syncthreads();
+  return s.n;
+}
+
 // Stretch of a range of `n` elements that a wavefront sums: whole loads of a wavefront, until the end.
 __device__ __forceinline__ int sample_stretch(int n) { return ((n + 15) / 16 + 255) / 256 * 256; }
 
@@ -392,7 +410,7 @@ __device__ __forceinline__ int sample_stretch(int n) { return ((n + 15) / 16 + 2
 // among the sorted members, and the token's stretch is known.  -2: the step holds more than the list, sample_cut finds the
 // prefix and sample_pick the token.  130001 logits: 240 us with sample_cut's exact histogram and sample_pick, 94 so.
 template <typename C, typename T>
-__device__ int sample_top_p(sample_lds& s, sample_row& r, C&& cut_of, T&& target_of) {
+__device__ int sample_top_p(sample_lds& s, sample_row& r, bool first, C&& cut_of, T&& target_of) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __syncthreads();
   s.list[tid] = 0;
@@ -400,7 +418,7 @@ __device__ int sample_top_p(sample_lds& s, sample_row& r, C&& cut_of, T&& target
   __syncthreads();
   const float c32 = (float)fmin(r.c, 1e38);
   const bool all = r.tau == 0 && r.tau_idx == 0xffffffffu;   // no prefix yet
-  for_each<4>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
+  for_each<2>(r.x, 0, r.V, tid, 1024, [&](int i, float v) {
     const float x = v == r.max ? r.top : r.infinite ? -INFINITY : v;
     float w = __builtin_amdgcn_exp2f(fmaxf((x - r.top) * c32, -126.0f));
     if (!all) w = r.in_prefix(key_of(v), i) ? w : 0.f;
@@ -452,6 +470,7 @@ __device__ int sample_top_p(sample_lds& s, sample_row& r, C&& cut_of, T&& target
     __syncthreads();
     r.tau = ~(uint32_t)(s.value >> 32);
     r.tau_idx = (uint32_t)s.value;
+    if (first) return sample_first(s, r);
 #pragma unroll
     for (int j = 0; j < 2; ++j)   // kept members join their stretch
       if (w[j] >= r.least && (j == 0 ? start : start + w[0]) < cut) atomicAdd(&s.wave[(int)(uint32_t)e[j] / len], w[j]);
@@ -460,16 +479,16 @@ __device__ int sample_top_p(sample_lds& s, sample_row& r, C&& cut_of, T&& target
 #pragma unroll
     for (int q = 0; q < 16; ++q) kept += s.wave[q];
     const u64 t = target_of(kept);
-    u64 run = 0, first = 0;
+    u64 run = 0, start_of = 0;
     int at = 0;
 #pragma unroll
     for (int q = 0; q < 16; ++q) {   // the last stretch whose start the target reaches
-      if (run <= t && s.wave[q] > 0) { at = q; first = run; }
+      if (run <= t && s.wave[q] > 0) { at = q; start_of = run; }
       run += s.wave[q];
     }
     __syncthreads();
     const int from = min(r.V, at * len);
-    return sample_pick_in(s, r, from, min(r.V, from + len), true, t - first, [&](int i, float v) {
+    return sample_pick_in(s, r, from, min(r.V, from + len), true, t - start_of, [&](int i, float v) {
       const u64 x = r.weight(v);
       return x >= r.least && r.in_prefix(key_of(v), i) ? x : (u64)0;
     }, [](u64 x) { return x; });
@@ -480,7 +499,7 @@ __device__ int sample_top_p(sample_lds& s, sample_row& r, C&& cut_of, T&& target
 __device__ void sample_extremes(sample_lds& s, const float* x, int lo, int hi, float* largest, float* smallest) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   float mx = -INFINITY, mn = INFINITY;
-  for_each<4>(x, lo, hi, tid, 1024, [&](int, float v) {
+  for_each<2>(x, lo, hi, tid, 1024, [&](int, float v) {
     mx = fmaxf(mx, v);
     mn = fminf(mn, v > -INFINITY ? v : INFINITY);
   });
@@ -510,6 +529,7 @@ __device__ __forceinline__ sample_row sample_load_row(const pt_sample_args& a, i
   r.c = 1.4426950408889634 / (double)temperature;
   r.tau = 0;
   r.tau_idx = 0xffffffffu;
+  r.min_p = min_p;
   r.least = min_p > 0.0f ? max((u64)1, (u64)fmin(ceil(ldexp((double)min_p, r.S)), ldexp(1.0, r.S))) : 1;
   return r;
 }
@@ -637,7 +657,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
     }
     if (tid == 0) s.n = 0x7fffffff;
     __syncthreads();
-    for_each<4>(r.x, lo, hi, tid, 1024, [&](int i, float v) {
+    for_each<2>(r.x, lo, hi, tid, 1024, [&](int i, float v) {
       if (v == r.max) atomicMin(&s.n, i);
     });
     __syncthreads();
@@ -650,7 +670,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
   auto target = [&](u64 total) { return min((u64)(u * (double)total), total - 1); };
   auto cut_mass = [&](u64 total) { return max((u64)1, min((u64)ceil(fmax((double)top_p, 0.0) * (double)total), total)); };
   if constexpr (PARTS) {
-    if (!k_on && !p_on && !(min_p > 0.0f)) {
+    if (!k_on && !p_on && !(min_p > 0.0f) && u > 0.0) {
       const int token = sample_from_sums(s, r, parts, a, u);
       if (tid == 0) a.out[row] = token;
       return;
@@ -707,6 +727,14 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
       u64 c = wave_scan64(w);
       u64 total = (u64)__shfl((long long)c, 63, 64);
       const u64 need = p_on ? cut_mass(total) : total;
+      if (u == 0.0) {   // see sample_first
+        const bool in = lane < m && r.has_weight(of_key(~(uint32_t)(e >> 32))) && (!p_on || c - w < need);
+        int token = in ? (int)(uint32_t)e : 0x7fffffff;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) token = min(token, __shfl_xor(token, o, 64));
+        if (lane == 0) a.out[row] = token;
+        return;
+      }
       if (!(w >= r.least && c - w < need)) {   // least is 1 or more: lanes without an element go too
         e = ~0ull;
         w = 0;
@@ -735,6 +763,19 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
       u64 total;
       const u64 c = block_scan64(s, w[0] + w[1], &total), start = c - w[0] - w[1];
       const u64 need = p_on ? cut_mass(total) : total;
+      if (u == 0.0) {   // see sample_first
+        if (tid == 0) s.n = 0x7fffffff;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int i = 2 * tid + j;
+          if (i < m && r.has_weight(of_key(~(uint32_t)(e[j] >> 32))) && (!p_on || (j == 0 ? start : start + w[0]) < need))
+            atomicMin(&s.n, (int)(uint32_t)e[j]);
+        }
+        __syncthreads();
+        if (tid == 0) a.out[row] = s.n;
+        return;
+      }
       // kept: in front of the target, and heavy enough; back into the list in order of index
       if (tid == 0) s.n = 0;
       __syncthreads();
@@ -773,7 +814,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
   if (p_on) {
     // mass lies within 40 T of the largest logit; the last step takes what is behind
     r.bin_scale = span > 0.0f ? (SAMPLE_BINS - 1) / fminf(span, 40.0f * temperature) : 0.0f;
-    const int token = sample_top_p(s, r, cut_mass, target);
+    const int token = sample_top_p(s, r, u == 0.0, cut_mass, target);
     if (token != -2) {
       if (tid == 0) a.out[row] = token;
       return;
@@ -781,7 +822,9 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
     sample_cut<false>(s, r, cut_mass);
   }
   int token;
-  if (!k_on && !p_on) {
+  if (u == 0.0) {
+    token = sample_first(s, r);
+  } else if (!k_on && !p_on) {
     token = sample_pick(s, r, [&](int, float v) {
       const u64 w = r.weight(v);
       return w >= r.least ? w : (u64)0;

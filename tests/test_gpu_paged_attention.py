@@ -188,6 +188,21 @@ def test_in_place():
     assert torch.equal(p.q[:used], want[:used]) and torch.equal(p.q[used:], keep[used:])
 
 
+@pytest.mark.parametrize("G", [1, 4])
+def test_in_place_before_a_position_that_is_no_number(G):
+    """The rows in front of it are computed anew from their queries, which lie where the output goes."""
+    p = Problem(2 * G, 2, 64, "bf16", 16, [(60, 90), (1, 30), (3, 20)], seed=20)
+    for b in (0, 2):
+        last = int(p.kv_len[b]) - 1
+        p.v5[p.layer, p.table[b, last // 16], :, last % 16] = float("nan")
+    want = p.run()
+    used = int(p.row_start[-1])
+    p.PB.pt_paged_attention(p.cache, p.layer, p.batch, p.q, out=p.q)
+    got = p.q[:used].float()
+    assert torch.equal(torch.isnan(got), torch.isnan(want[:used].float())) and not torch.isnan(got[:59]).any()
+    assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want[:used].float()))
+
+
 def test_pages_that_do_not_exist_are_reported():
     p = Problem(4, 2, 64, "bf16", 16, [(1, 40), (1, 40)], seed=13)
     want = p.run()

@@ -117,6 +117,22 @@ def test_extreme_temperatures():
     assert draw(x, [0.0, 0.5, 0.5, 0.9995], [INF] * 4).tolist() == [0, 1000, 1000, 1998]
 
 
+@pytest.mark.parametrize("vocab", [50, 3000, 40000, 70001])
+def test_a_uniform_number_of_zero_takes_the_first_token_with_any_weight(vocab):
+    """However light it is: 2^-60 of the largest, or 2^-900, but not what fp64 cannot hold."""
+    x = np.full((8, vocab), -2000.0, np.float32)
+    x[:, vocab // 2] = 10.0
+    for r, (i, v) in enumerate(((7, -30.0), (3, -600.0), (9, -800.0), (0, 9.0))):
+        x[r, i] = x[r + 4, i] = v
+    k, p, m = [0, 5, 3, 2] * 2, [1.0] * 8, [0.0] * 8
+    check(x, [0.0] * 8)
+    check(x, [0.0] * 8, k=k)
+    check(x, [0.0] * 8, k=[700] * 8)
+    check(x, [0.0] * 8, p=[0.999] * 4 + [0.3] * 4)
+    check(x, [0.0] * 8, k=k, p=[0.999] * 4 + [0.3] * 4, m=[0.0, 0.0, 1e-6, 0.1] * 2)
+    check(x, [0.0] * 8, m=[1e-25] * 4 + [0.2] * 4)
+
+
 def test_rows_apart_and_unaligned():
     rng = np.random.default_rng(6)
     for off in (0, 1, 2, 3):
