@@ -27,10 +27,16 @@ __device__ __forceinline__ void static_for(F&& f) {
 
 // Largest of the four lanes that share lane % 16.
 __device__ __forceinline__ float max_over_groups(float v) {
+  // fmaxf would first pass each exchanged value through an instruction of its own
+  auto larger = [](uint32_t x, uint32_t y) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+    return r;
+  };
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  v = larger(a[0], a[1]);
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+  return larger(b[0], b[1]);
 }
 
 constexpr int PA_MAX_SPLITS = 64;   // a wavefront of the combine holds one range's statistics per lane
@@ -214,6 +220,8 @@ __device__ __forceinline__ void paged_merge(const pt_paged_attn_args& a, const p
 // (16 lanes read a 4 x 16 block and receive its columns).
 // MFMA contraction order of the second product: lane group g holds, of 32 keys, 4g..4g+3 of the first and of the second
 // 16 - what the S^T result leaves in its registers, and what two transposing reads deliver.
+// What bounds it is HBM: 64 sequences of 128 to 8192 keys on 16 KV heads of 128, 2.19 GB, 378 us = 5.8 TB/s where a streaming read
+// reaches 6.0 to 6.2; tiles of 32 keys instead of 64 there 399.  One workgroup holds 128 KB of tiles at hd = 128.
 // NQ: blocks of 16 packed rows.  FULL: hd == HD; otherwise the rest of the LDS rows is zeroed once and never loaded.
 // ------------------------------------------------------------------------------------------------
 template <int HD>
@@ -479,7 +487,15 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
 // ------------------------------------------------------------------------------------------------
 // bf16, many rows: four wavefronts of 32 packed rows each share key tiles of 64 (K and V as they lie in their pages, two
 // tiles in LDS: one that is read, one on its way).  A wavefront loads the tile's 16 keys of its number - one page - and
-// multiplies all 64 with its own rows; MFMA layouts, swizzle and transposing reads as above.
+// multiplies all 64 with its own rows; MFMA layouts, swizzle and transposing reads as above.  The rows' sums of probabilities
+// are one more product, with a row of ones: it costs matrix time that is free and saves as much vector time as the maximum.
+// What bounds it: 2048 rows over 16384 keys, 64 heads on 8 KV heads of 128, 1.03 TFLOP, 945 us = 1.09 PFLOP/s; matrix pipes
+// busy 51 % and vector issue 61 % of the time at 2.0 GHz.  On zeros the same call takes 851 us (the chip gives way with its
+// clock on data); without loads into LDS 840, without the exponentials 795, without LDS reads of operands 857.  Steps:
+// no overlap inside a wavefront 1058, units of 32 keys in three stages (below) 955, sums by product 940.  Measured and not
+// kept: 64 rows per wavefront, one to a SIMD (1133: scores travel between accumulation and vector registers), eight
+// wavefronts to a tile (no change), the search for the maximum spread over the second product (no change at 128, 10 %
+// slower at 64), two or eight fragments in flight instead of four (no change).
 // ------------------------------------------------------------------------------------------------
 template <int HD, bool FULL>
 __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int block, char* smem) {   // smem: [2][K tile], [2][V tile]
@@ -562,12 +578,13 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
   for (int hb = 0; hb < HB; ++hb) va[hb] = lds0 + 2 * TILE_B + vrow * ROWB + (((hb * 2 + ((l16 & 3) >> 1)) ^ geo::swz(vrow)) * 16) + (l16 & 1) * 8;
   typedef const __attribute__((address_space(3))) bf16x8_t* lk_t;
 
-  f32x4_t acc[NQ][HB];
-  float m_run[NQ], l_run[NQ];
+  f32x4_t acc[NQ][HB], l_run[NQ];   // l_run: the rounded probabilities' sums, the product with a row of ones
+  float m_run[NQ];
+  const bf16x8_t ones = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     m_run[n] = -INFINITY;
-    l_run[n] = 0.f;
+    l_run[n] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) acc[n][hb] = {0.f, 0.f, 0.f, 0.f};
   }
@@ -640,12 +657,11 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
                   uint32_t v_at, uint32_t k_next, int first) __attribute__((always_inline)) {
     constexpr bool LAG = decltype(LAG_)::value, NEXT = decltype(NEXT_)::value;
     constexpr int END = LAG ? STEPS : NS;
-    float mc[NQ], top[NQ], psum[NQ];
+    float mc[NQ], top[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       mc[n] = m_run[n] == -INFINITY ? 0.f : m_run[n];
       top[n] = -INFINITY;
-      psum[n] = 0.f;
     }
     // One MFMA at a time, and behind it its share of the scores: what a wavefront issues right behind an MFMA runs beside it,
     // another MFMA would wait for the first one's end.
@@ -659,6 +675,7 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
         s_nxt[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i % PF].v, qf[n][kk], s_nxt[n][b], 0, 0, 0);
       } else {
         acc[n][i - NS] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[i % PF].v, p_old[n].v, acc[n][i - NS], 0, 0, 0);
+        if constexpr (i == NS) l_run[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p_old[n].v, l_run[n], 0, 0, 0);
       }
       if constexpr (n == NQ - 1 && i + PF < END) fetch(std::integral_constant<int, i + PF>{}, k_at, v_at);
       if constexpr (n == NQ - 1 && i + PF >= END && NEXT) fetch(std::integral_constant<int, i + PF - END>{}, k_next, 0);
@@ -667,14 +684,13 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
         if constexpr (sc * SLOTS / SCORES == slot) {   // score: query block, key block, register
           constexpr int n = sc / (UB * 4), b = sc / 4 % UB, v = sc % 4;
           float p = __builtin_amdgcn_exp2f(fmaf(s_cur[n][b][v], c_log2, -mc[n]));
-          psum[n] += p;
           // formed here: the compiler would move all of it behind the last product otherwise
           if constexpr (v % 2 == 0) {
-            asm volatile("" : "+v"(p), "+v"(psum[n]));
+            asm volatile("" : "+v"(p));
             half[n] = p;
           } else {
             p_new[n].u[2 * b + v / 2] = pack_bf16x2(half[n], p);
-            asm volatile("" : "+v"(p_new[n].u[2 * b + v / 2]), "+v"(psum[n]));
+            asm volatile("" : "+v"(p_new[n].u[2 * b + v / 2]));
           }
         }
       });
@@ -683,7 +699,6 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
     mask_unit(s_nxt, first + UK);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      l_run[n] += psum[n];
 #pragma unroll
       for (int b = 0; b < UB; ++b)
 #pragma unroll
@@ -770,8 +785,7 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
   // acc[n][hb], register v: element 16 hb + 4 g + v of query n * 16 + l16
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    float l = l_run[n] + __shfl_xor(l_run[n], 16, 64);
-    l += __shfl_xor(l, 32, 64);
+    const float l = l_run[n][0];
     const float m = m_run[n];
     const int r = t.row0 + w0 + n * 16 + l16, i = r / G, head = kvh * G + (r - i * G), row = t.sq.first + i;
     const bool real = w0 + n * 16 + l16 < t.nrows;
@@ -834,7 +848,9 @@ __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_
 
 // Decode steps beside chunks in one launch: workgroups of the one kind wait for HBM while those of the other multiply.  Stretches
 // of 64 workgroups are dealt to the two kinds in proportion (multiples of the 8 XCDs, so that a KV head stays on its own).
-// Two workgroups share a compute unit: the few rows' tiles hold half the keys at hd = 128.
+// Two workgroups share a compute unit: the few rows' tiles hold half the keys at hd = 128.  36 decode steps and 4 chunks of
+// 400 on 64 heads of 64: 179 us, one kernel behind the other 118 + 72; more of it needs more workgroups to a unit than 159
+// registers leave (tiles of 32 keys, three workgroups: 182 to 192).
 constexpr int PA_DEAL = 64;
 template <int HD, bool FULL>
 __global__ void __launch_bounds__(256, 2) paged_attn_both_kernel(const pt_paged_attn_args a, int many, int few) {
@@ -852,7 +868,7 @@ __global__ void __launch_bounds__(256, 2) paged_attn_both_kernel(const pt_paged_
 }
 
 // ------------------------------------------------------------------------------------------------
-// fp32, on 16x16x4 MFMAs: 16 packed rows per workgroup, 16 keys per wavefront and step, operands straight from the pages.
+// fp32 (latency and L2 bound at the sizes it is for), on 16x16x4 MFMAs: 16 packed rows per workgroup, 16 keys per wavefront and step, operands straight from the pages.
 // The contraction over the head takes elements 16 j + 4 g + i in step (j, i), so that a lane's operands are 16-byte loads; the
 // second product's rows are head elements 64 hb + 4 r + j for the same reason.
 // ------------------------------------------------------------------------------------------------

@@ -42,12 +42,13 @@ def attention_bound(ref, weight, score, hd, keys, bf16):
     """How far a right result may be off, element by element.  Scores: a sum of hd products in fp32 and two more roundings,
     so their error is at most (hd + 2) * 2^-24 * sum|q k|; the reference of the exponents and its product add two steps
     of the largest score each, the exponential four; an error d of a score changes a weight by the factor exp(2 d) at most
-    (its own and the normalisation's).  The weighted sum adds `keys` steps.  bf16: one rounding per probability, which the
-    normalisation does not share, and one of the result."""
+    (its own and the normalisation's).  The weighted sum adds `keys` steps.  bf16: one rounding per probability, and one of
+    the result.  Where the sum that normalises is that of the rounded probabilities p (1 + e), |e| <= 2^-8, the result is off
+    by sum p e (v - out) / sum p (1 + e): at most 2^-8 (sum p |v| + |out|) and a factor 1 / (1 - 2^-8)."""
     d = (hd + 2) * FP32_STEP * score + 4 * FP32_STEP * score + 4 * FP32_STEP
     tol = weight * (np.expm1(2 * d) + (2 * keys + 8) * FP32_STEP)
     if bf16:
-        tol = tol + weight * BF16_STEP
+        tol = tol + (weight + np.abs(ref)) * BF16_STEP / (1 - BF16_STEP)
     return tol + (np.abs(ref) + tol) * (BF16_STEP if bf16 else FP32_STEP) + 1e-37
 
 
