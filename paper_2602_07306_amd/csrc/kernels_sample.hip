@@ -138,31 +138,71 @@ __device__ __forceinline__ void for_each(const float* x, int lo, int hi, int tid
   if (i >= 0) f(i, x[i]);
 }
 
+// Lanes exchange through the vector unit's own paths (moves within rows of 16, swaps of rows and halves) and not through LDS,
+// whose latency would be that of every step of a scan or sort.
+template <int CTRL, int BANKS = 0xf>
+__device__ __forceinline__ uint32_t dpp(uint32_t old, uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, 0xf, BANKS, false);
+}
+constexpr int DPP_QUAD_SWAP1 = 0xb1, DPP_QUAD_SWAP2 = 0x4e, DPP_ROW_SHL = 0x100, DPP_ROW_SHR = 0x110, DPP_ROW_ROR = 0x120;
+
+// The value of lane ^ J.
+template <int J>
+__device__ __forceinline__ uint32_t partner32(uint32_t v) {
+  if constexpr (J == 1) return dpp<DPP_QUAD_SWAP1>(v, v);
+  if constexpr (J == 2) return dpp<DPP_QUAD_SWAP2>(v, v);
+  if constexpr (J == 4) return dpp<DPP_ROW_SHR + 4, 0xa>(dpp<DPP_ROW_SHL + 4, 0x5>(v, v), v);
+  if constexpr (J == 8) return dpp<DPP_ROW_ROR + 8>(v, v);
+  if constexpr (J == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  }
+  if constexpr (J == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? r[0] : r[1];
+  }
+}
+template <int J>
+__device__ __forceinline__ u64 partner64(u64 v) {
+  return (u64)partner32<J>((uint32_t)(v >> 32)) << 32 | partner32<J>((uint32_t)v);
+}
+template <int J>
+__device__ __forceinline__ void sum_step(u64& v) { v += partner64<J>(v); }
 __device__ __forceinline__ u64 wave_sum64(u64 v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += (u64)__shfl_xor((long long)v, o, 64);
+  sum_step<1>(v); sum_step<2>(v); sum_step<4>(v); sum_step<8>(v); sum_step<16>(v); sum_step<32>(v);
   return v;
+}
+template <int N>
+__device__ __forceinline__ void scan_step(u64& v) {   // plus the value N lanes before, inside a row
+  v += (u64)dpp<DPP_ROW_SHR + N>(0, (uint32_t)(v >> 32)) << 32 | dpp<DPP_ROW_SHR + N>(0, (uint32_t)v);
+}
+__device__ __forceinline__ u64 lane_value64(u64 v, int lane) {   // lane: the same everywhere
+  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
 __device__ __forceinline__ u64 wave_scan64(u64 v) {   // inclusive
   const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64 up = (u64)__shfl_up((long long)v, o, 64);
-    if (lane >= o) v += up;
-  }
-  return v;
+  scan_step<1>(v); scan_step<2>(v); scan_step<4>(v); scan_step<8>(v);
+  const u64 r0 = lane_value64(v, 15), r1 = lane_value64(v, 31), r2 = lane_value64(v, 47);
+  return v + (lane >= 48 ? r0 + r1 + r2 : lane >= 32 ? r0 + r1 : lane >= 16 ? r0 : 0);
 }
-// The wavefront's values in ascending order of lanes.
-__device__ __forceinline__ u64 wave_sort64(u64 v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      const u64 o = (u64)__shfl_xor((long long)v, j, 64);
-      const bool low = (lane & j) == 0, up = (lane & k) == 0;
-      v = (v < o) == (low == up) ? v : o;
-    }
+// One step of a bitonic sort: `index` is compared with index ^ J, ascending where `up`.
+template <int J>
+__device__ __forceinline__ void sort_step(u64& v, bool up) {
+  const u64 o = partner64<J>(v);
+  v = (v < o) == (((threadIdx.x & J) == 0) == up) ? v : o;
+}
+__device__ __forceinline__ void sort_merge32(u64& v, bool up) {   // steps of 32 and less
+  sort_step<32>(v, up); sort_step<16>(v, up); sort_step<8>(v, up); sort_step<4>(v, up); sort_step<2>(v, up); sort_step<1>(v, up);
+}
+// The wavefront's values in ascending order of lanes, or descending.
+__device__ __forceinline__ u64 wave_sort64(u64 v, bool up = true) {
+  const int lane = threadIdx.x;
+  sort_step<1>(v, !(lane & 2));
+  sort_step<2>(v, !(lane & 4)); sort_step<1>(v, !(lane & 4));
+  sort_step<4>(v, !(lane & 8)); sort_step<2>(v, !(lane & 8)); sort_step<1>(v, !(lane & 8));
+  sort_step<8>(v, !(lane & 16)); sort_step<4>(v, !(lane & 16)); sort_step<2>(v, !(lane & 16)); sort_step<1>(v, !(lane & 16));
+  sort_step<16>(v, !(lane & 32)); sort_step<8>(v, !(lane & 32)); sort_step<4>(v, !(lane & 32)); sort_step<2>(v, !(lane & 32)); sort_step<1>(v, !(lane & 32));
+  sort_merge32(v, up);
   return v;
 }
 // Inclusive sum over the workgroup's threads; *total the whole.
@@ -232,21 +272,54 @@ __device__ int sample_pick(sample_lds& s, const sample_row& r, W&& weight, T&& t
   return sample_pick_in(s, r, 0, r.V, false, 0, weight, target);
 }
 
-// Sorts s.list[0 .. n-1] ascending; padded to a power of two with the largest value.
+// Sorts s.list[0 .. n-1] ascending (bitonic; padded with the largest value to a power of two, 64 at least).  A thread holds the elements
+// tid and, of more than 1024, tid + 1024: steps of less than 64 stay in the wavefronts' registers, wider ones go through
+// LDS, 10 of 55 for 1024 elements.
 __device__ void sample_sort(sample_lds& s, int n) {
-  int size = 2;
+  const int tid = threadIdx.x;
+  int size = 64;
   while (size < n) size <<= 1;
-  for (int i = n + threadIdx.x; i < size; i += 1024) s.list[i] = ~0ull;
-  for (int k = 2; k <= size; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
+  const bool busy = (tid & ~63) < size;   // wavefront-uniform
+  u64 v[2];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int i = tid + 1024 * e;
+    v[e] = i < n ? s.list[i] : ~0ull;
+    if (busy) v[e] = wave_sort64(v[e], size == 64 || !(i & 64));
+  }
+  for (int k = 128; k <= size; k <<= 1) {
+    for (int j = k >> 1; j >= 64; j >>= 1) {
+      if (j == 1024) {
+        const u64 a = min(v[0], v[1]);
+        v[1] = max(v[0], v[1]);
+        v[0] = a;
+        continue;
+      }
       __syncthreads();
-      const int p = threadIdx.x;
-      if (p < size / 2) {
-        const int i = 2 * p - (p & (j - 1)), l = i + j;
-        const u64 a = s.list[i], b = s.list[l];
-        if ((a > b) == ((i & k) == 0)) { s.list[i] = b; s.list[l] = a; }
+      if (busy) {
+        s.list[tid] = v[0];
+        if (size > 1024) s.list[tid + 1024] = v[1];
+      }
+      __syncthreads();
+      if (busy) {
+        const bool low = (tid & j) == 0;
+        u64 o = s.list[tid ^ j];
+        v[0] = (v[0] < o) == (low == ((tid & k) == 0)) ? v[0] : o;
+        if (size > 1024) {
+          o = s.list[(tid ^ j) + 1024];
+          v[1] = (v[1] < o) == (low == (((tid + 1024) & k) == 0)) ? v[1] : o;
+        }
       }
     }
+    if (busy) {
+      sort_merge32(v[0], (tid & k) == 0);
+      if (size > 1024) sort_merge32(v[1], ((tid + 1024) & k) == 0);
+    }
+  }
+  __syncthreads();
+  if (tid < size) s.list[tid] = v[0];
+  if (size > 1024) s.list[tid + 1024] = v[1];
   __syncthreads();
 }
 
@@ -680,9 +753,18 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
     }
   }
 
-  if (k_on && top_k <= SAMPLE_LIST_K) {
+  // Among a list: the candidates for a small k, or all of a short row.
+  const bool short_row = r.V <= SAMPLE_LIST && (k_on || p_on);
+  if (short_row || (k_on && top_k <= SAMPLE_LIST_K)) {
+    const int most = k_on ? top_k : r.V;   // how many of the list count
     int n = SAMPLE_LIST + 1;
-    if (PARTS && top_k <= SAMPLE_PART_K) {
+    if (short_row) {
+      n = r.V;
+      __syncthreads();
+      for (int i = tid; i < n; i += 1024) s.list[i] = (u64)~key_of(r.x[i]) << 32 | (uint32_t)i;
+      __syncthreads();
+    }
+    if (PARTS && !short_row && top_k <= SAMPLE_PART_K) {
       // the parts' candidates, one part behind the other
       const int own = lane < a.parts ? max(parts[lane].n, 0) : 0;
       const bool whole = __all(own <= SAMPLE_PART_LIST);
@@ -707,7 +789,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
       const float bound = sample_bound(s, top_k);
       n = sample_gather(s, r, 0, r.V, [&](int, float v) { return v >= bound && v > -INFINITY; });
     }
-    if (n > 64 && n <= 512 && top_k <= 64) {
+    if (n > 64 && n <= 512 && most <= 64) {
       // the k largest by comparing each with all: the sorts below have a barrier per step
       const u64 mine = tid < n ? s.list[tid] : ~0ull;
       int rank = 0;
@@ -716,19 +798,19 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
         for (int j = 0; j < n; ++j) rank += s.list[j] < mine;
       }
       __syncthreads();
-      if (tid < n && rank < top_k) s.list[rank] = mine;
+      if (tid < n && rank < most) s.list[rank] = mine;
       __syncthreads();
-      n = top_k;
+      n = most;
     }
     if (n <= 64) {
       // one wavefront, an element per lane: the same steps without a barrier
       if (wave > 0) return;
       u64 e = lane < n ? s.list[lane] : ~0ull;
       e = wave_sort64(e);
-      const int m = min(n, top_k);
+      const int m = min(n, most);
       u64 w = lane < m ? r.weight(of_key(~(uint32_t)(e >> 32))) : 0;
       u64 c = wave_scan64(w);
-      u64 total = (u64)__shfl((long long)c, 63, 64);
+      u64 total = lane_value64(c, 63);
       const u64 need = p_on ? cut_mass(total) : total;
       if (u == 0.0) {   // see sample_first
         const bool in = lane < m && r.has_weight(of_key(~(uint32_t)(e >> 32))) && (!p_on || c - w < need);
@@ -747,7 +829,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
       e = wave_sort64(e);
       w = e != ~0ull ? r.weight(of_key((uint32_t)e)) : 0;
       c = wave_scan64(w);
-      total = (u64)__shfl((long long)c, 63, 64);
+      total = lane_value64(c, 63);
       const u64 t = target(total);
       if (w > 0 && c - w <= t && c > t) a.out[row] = (int32_t)(e >> 32);
       return;
@@ -755,7 +837,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
     if (n <= SAMPLE_LIST) {
       sample_sort(s, n);
       // two elements per thread, in order; those past k drop out
-      const int m = min(n, top_k);
+      const int m = min(n, most);
       u64 e[2], w[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
