@@ -478,10 +478,10 @@ __device__ __forceinline__ void paged_few_rows(const pt_paged_attn_args& a, int 
 #endif
 }
 
-template <int HD, int NQ, bool FULL>
+template <int HD, int NQ, bool FULL, int TK>
 __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_args a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  paged_few_rows<HD, NQ, FULL, HD == 256 ? 32 : 64>(a, blockIdx.x, smem);
+  paged_few_rows<HD, NQ, FULL, TK>(a, blockIdx.x, smem);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -985,44 +985,70 @@ __global__ void __launch_bounds__(256, 1) paged_attn_f32_kernel(const pt_paged_a
   paged_merge<float, HD>(a, t, split, kvh, k0, k1, red_o, red_ml);
 }
 
-// Joins the ranges of a tile's rows, a row per wavefront at a time and in the ranges' order; 16 rows per workgroup.  Tiles whose
-// keys fitted one range are done already.
-template <typename T, bool WIDE>
-__global__ void __launch_bounds__(256) paged_combine_kernel(const pt_paged_attn_args a) {
+// Joins the ranges of a tile's rows, in the ranges' order.  Tiles whose keys fitted one range are done already.  A wavefront takes a
+// row, four rows a workgroup; many ranges (SHARE = 4) are shared out to a workgroup's wavefronts, which read eight at a time
+// (one sequence of 16000 keys in 63 ranges, attention and joining: 96 us with a wavefront to a row, one range after the other; 29).
+template <typename T, bool WIDE, int SHARE>
+__device__ __forceinline__ void paged_combine(const pt_paged_attn_args& a, int block, float (*shared)[256]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const pt_paged_cut& cut = a.cut[WIDE];
-  const int parts = cut.tile_rows / 16, G = a.H / a.Hkv;
-  const int kvh = blockIdx.x % a.Hkv;
-  const int rest = blockIdx.x / a.Hkv;
+  const int parts = cut.tile_rows / (4 / SHARE), G = a.H / a.Hkv;
+  const int kvh = block % a.Hkv;
+  const int rest = block / a.Hkv;
   paged_tile t;
   if (!paged_find_tile<WIDE>(a, rest / parts, &t) || t.nsplit == 1) return;
-  const int r0 = rest % parts * 16;
+  const int r = rest % parts * (4 / SHARE) + (SHARE == 4 ? 0 : wave);
+  if (r >= t.nrows) return;                         // SHARE = 4: all four wavefronts alike
   const int64_t step = (int64_t)a.b.total_rows * a.H;
-  for (int r = r0 + wave; r < min(r0 + 16, t.nrows); r += 4) {
-    const int i = (t.row0 + r) / G, head = kvh * G + (t.row0 + r) - i * G, row = t.sq.first + i;
-    const int64_t at = (int64_t)row * a.H + head;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < t.nsplit) ml = a.part_ml[lane * step + at];
-    const float m = wave_max(ml.x);
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-    const float l = wave_sum(f * ml.y);
-    const int lim = paged_vis(a, t.sq, i);
-    for (int e = lane; e < a.hd; e += 64) {
-      float o = 0.f;
-#pragma unroll 4
-      for (int s = 0; s < t.nsplit; ++s) o += __shfl(f, s, 64) * a.part_o[(s * step + at) * a.hd + e];
-      elem<T>::st((T*)a.o + row * a.o_rs + head * a.o_hs + e, lim <= 0 ? 0.f : o / l);
+  const int i = (t.row0 + r) / G, head = kvh * G + (t.row0 + r) - i * G, row = t.sq.first + i;
+  const int64_t at = (int64_t)row * a.H + head;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (lane < t.nsplit) ml = a.part_ml[lane * step + at];
+  const float m = wave_max(ml.x);
+  const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+  const float l = wave_sum(f * ml.y);
+  const int lim = paged_vis(a, t.sq, i);
+  // a wavefront's ranges: consecutive ones
+  const int per = (t.nsplit + SHARE - 1) / SHARE, s0 = SHARE == 4 ? min(t.nsplit, wave * per) : 0, s1 = min(t.nsplit, s0 + per);
+  float o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = s0; s < s1; s += 8) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float fs = __shfl(f, min(s + u, 63), 64);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (s + u < s1 && lane + 64 * j < a.hd) o[j] += fs * a.part_o[((s + u) * step + at) * a.hd + lane + 64 * j];
     }
   }
+  if constexpr (SHARE == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) shared[wave][lane + 64 * j] = o[j];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = ((shared[0][lane + 64 * j] + shared[1][lane + 64 * j]) + shared[2][lane + 64 * j]) + shared[3][lane + 64 * j];
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (lane + 64 * j < a.hd) elem<T>::st((T*)a.o + row * a.o_rs + head * a.o_hs + lane + 64 * j, lim <= 0 ? 0.f : o[j] / l);
+}
+
+// The first `few` workgroups join tiles of few rows, the others those of many.
+template <typename T, int SHARE>
+__global__ void __launch_bounds__(256) paged_combine_kernel(const pt_paged_attn_args a, int few) {
+  __shared__ float shared[4][256];
+  if ((int)blockIdx.x < few) paged_combine<T, false, SHARE>(a, blockIdx.x, shared);
+  else paged_combine<T, true, SHARE>(a, blockIdx.x - few, shared);
 }
 
 constexpr int PA_WIDE_ROWS = 128;
 
-// Ranges of keys for `units` workgroups: as many as it takes to have `want` of them, each of at least 256 keys (a tile of 64 for
-// every wavefront).  One range where `single` keys are not exceeded: one sequence of 777 keys, 64 heads of 64, takes 8.5 us
-// in one and 5.4 + 3.9 in four with the launch that joins them.
-static void paged_ranges(int64_t units, int64_t keys, int64_t want, int64_t single, pt_paged_cut* c) {
-  int64_t splits = keys <= single ? 1 : std::min<int64_t>((want + units - 1) / units, PA_MAX_SPLITS);
+// Ranges of keys for `units` workgroups: as many as it takes to have 512 of them, two to a compute unit, each of at least 256 keys (a
+// tile of 64 for every wavefront) and at most `longest`.  One range where `single` keys are not exceeded: one sequence of
+// 777 keys, 64 heads of 64, takes 8.5 us in one and 5.4 + 3.9 in four with the launch that joins them.
+static void paged_ranges(int64_t units, int64_t keys, int64_t single, int64_t longest, pt_paged_cut* c) {
+  int64_t splits = keys <= single ? 1 : std::max((512 + units - 1) / units, (keys + longest - 1) / longest);
+  splits = std::min<int64_t>(splits, PA_MAX_SPLITS);
   const int64_t chunk = ((keys + splits - 1) / splits + 255) / 256 * 256;
   c->chunk = (int32_t)chunk;
   c->n_splits = (int32_t)((keys + chunk - 1) / chunk);
@@ -1048,11 +1074,13 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
   }
   p->cut[0].tiles = (int32_t)std::min<int64_t>(t0, 0x7fffffff);
   p->cut[1].tiles = (int32_t)std::min<int64_t>(t1, 0x7fffffff);
-  // Few rows: 2048 workgroups, so that sequences of different lengths even out (64 of 128 to 8192 keys on 16 KV heads: 387 us;
-  // 1024 workgroups, one range each, 383; 4096 395).  The fp32 kernel takes 64 keys at a time where the other takes 256.
-  if (t0 > 0) paged_ranges(t0 * Hkv, keys, 2048, dtype == PT_F32 ? 256 : 1024, &p->cut[0]);
-  if (t1 > 0) paged_ranges(t1 * Hkv, keys, 512, 256, &p->cut[1]);
-  if (t0 * Hkv * std::max(2, p->cut[0].n_splits) > 0x3fffffff || t1 * Hkv * std::max(8, p->cut[1].n_splits) > 0x3fffffff)
+  // Few rows, 2048 / 512 workgroups wanted, us: 23 sequences of 1324 to 5606 keys on 8 KV heads of 128 88 / 68, 60 of 1100 to 2000 on
+  // 16 169 / 137, 64 of 128 to 8192 on 16 387 / 383; past 8192 keys a range is cut all the same, so that one long sequence among
+  // short ones does not end as one workgroup.  The fp32 kernel takes 64 keys at a time where the other takes 256.
+  if (t0 > 0) paged_ranges(t0 * Hkv, keys, dtype == PT_F32 ? 256 : 1024, 8192, &p->cut[0]);
+  // Many rows: by the number of tiles that the rows make up, not its bound.
+  if (t1 > 0) paged_ranges((b.total_rows * G / PA_WIDE_ROWS + 1) * Hkv, keys, 256, keys, &p->cut[1]);
+  if (t0 * Hkv * std::max(32, p->cut[0].n_splits) > 0x3fffffff || t1 * Hkv * 128 > 0x3fffffff)
     return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
   const int32_t splits = std::max(p->cut[0].n_splits, p->cut[1].n_splits);
   if (splits > 1) {
@@ -1063,18 +1091,26 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
   return PT_OK;
 }
 
-template <int HD, int NQ, bool FULL>
+template <int HD, int NQ, bool FULL, int TK>
 static int launch_paged(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
-  constexpr int LDS = std::max(8 * (HD == 256 ? 32 : 64) * paged_geom<HD>::ROWB, 4 * 16 * NQ * ((HD + 4) * 4 + 8));
+  constexpr int LDS = std::max(8 * TK * paged_geom<HD>::ROWB, 4 * 16 * NQ * ((HD + 4) * 4 + 8));
   static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
-  auto kern = paged_attn_kernel<HD, NQ, FULL>;
+  auto kern = paged_attn_kernel<HD, NQ, FULL, TK>;
   PT_SET_MAX_LDS_ONCE(kern, LDS);
   hipLaunchKernelGGL(kern, dim3(grid), dim3(256), LDS, s, a);
   return PT_OK;
 }
-template <int HD, int NQ>
+template <int HD, int NQ, int TK>
 static int launch_paged_full(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
-  return a.hd == HD ? launch_paged<HD, NQ, true>(a, grid, s) : launch_paged<HD, NQ, false>(a, grid, s);
+  return a.hd == HD ? launch_paged<HD, NQ, true, TK>(a, grid, s) : launch_paged<HD, NQ, false, TK>(a, grid, s);
+}
+// Keys of a tile: 64, and 32 where that is 512 bytes a key.  At 256 bytes a key tiles of 64 leave room for one workgroup to a
+// compute unit, whose first loads and merge nothing covers; in ranges of up to 1024 keys that costs more than the smaller
+// tiles do (67 sequences of 208 to 338 keys on 8 KV heads of 128: 26 us against 20; of 8192 keys: 377 against 399).
+template <int HD, int NQ>
+static int launch_paged_tile(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
+  if constexpr (HD == 128) return a.cut[0].chunk <= 1024 ? launch_paged_full<128, NQ, 32>(a, grid, s) : launch_paged_full<128, NQ, 64>(a, grid, s);
+  else return launch_paged_full<HD, NQ, HD == 64 ? 64 : 32>(a, grid, s);
 }
 template <int HD>
 static int launch_paged_f32(const pt_paged_attn_args& a, unsigned grid, hipStream_t s) {
@@ -1089,12 +1125,6 @@ static int launch_wide(const pt_paged_attn_args& a, unsigned grid, hipStream_t s
   PT_SET_MAX_LDS_ONCE(kern, LDS);
   hipLaunchKernelGGL(kern, dim3(grid), dim3(256), LDS, s, a);
   return PT_OK;
-}
-
-template <typename T, bool WIDE>
-static void launch_combine(const pt_paged_attn_args& a, hipStream_t s) {
-  const unsigned blocks = (unsigned)((int64_t)a.cut[WIDE].tiles * a.Hkv * (a.cut[WIDE].tile_rows / 16));
-  hipLaunchKernelGGL((paged_combine_kernel<T, WIDE>), dim3(blocks), dim3(256), 0, s, a);
 }
 
 template <int HD, bool FULL>
@@ -1127,18 +1157,26 @@ int pt_launch_paged_attn(const pt_paged_attn_args& a, int32_t dtype, hipStream_t
     if (dtype == PT_F32) {
       rc = a.hd <= 64 ? launch_paged_f32<64>(a, grid, s) : a.hd <= 128 ? launch_paged_f32<128>(a, grid, s) : launch_paged_f32<256>(a, grid, s);
     } else if (a.hd <= 64) {
-      rc = nq == 1 ? launch_paged_full<64, 1>(a, grid, s) : launch_paged_full<64, 2>(a, grid, s);
+      rc = nq == 1 ? launch_paged_tile<64, 1>(a, grid, s) : launch_paged_tile<64, 2>(a, grid, s);
     } else if (a.hd <= 128) {
-      rc = nq == 1 ? launch_paged_full<128, 1>(a, grid, s) : launch_paged_full<128, 2>(a, grid, s);
+      rc = nq == 1 ? launch_paged_tile<128, 1>(a, grid, s) : launch_paged_tile<128, 2>(a, grid, s);
     } else {
-      rc = nq == 1 ? launch_paged_full<256, 1>(a, grid, s) : launch_paged_full<256, 2>(a, grid, s);
+      rc = nq == 1 ? launch_paged_tile<256, 1>(a, grid, s) : launch_paged_tile<256, 2>(a, grid, s);
     }
   }
   if (rc) return rc;
-  if (a.cut[1].n_splits > 1) launch_combine<bf16_t, true>(a, s);
-  if (a.cut[0].n_splits > 1) {
-    if (dtype == PT_F32) launch_combine<float, false>(a, s);
-    else launch_combine<bf16_t, false>(a, s);
+  const int share = std::max(a.cut[0].n_splits, a.cut[1].n_splits) > 8 ? 4 : 1;   // wavefronts to a row
+  auto joins = [&](int c) { return a.cut[c].n_splits > 1 ? a.cut[c].tiles * a.Hkv * (a.cut[c].tile_rows / (4 / share)) : 0; };   // workgroups
+  const int few = joins(0), many = joins(1);
+  if (few + many > 0) {
+    const dim3 grid((unsigned)(few + many));
+    if (dtype == PT_F32) {
+      if (share == 4) hipLaunchKernelGGL((paged_combine_kernel<float, 4>), grid, dim3(256), 0, s, a, few);
+      else hipLaunchKernelGGL((paged_combine_kernel<float, 1>), grid, dim3(256), 0, s, a, few);
+    } else {
+      if (share == 4) hipLaunchKernelGGL((paged_combine_kernel<bf16_t, 4>), grid, dim3(256), 0, s, a, few);
+      else hipLaunchKernelGGL((paged_combine_kernel<bf16_t, 1>), grid, dim3(256), 0, s, a, few);
+    }
   }
   PT_HIP_CHECK(hipGetLastError());
   return PT_OK;

@@ -4,9 +4,9 @@ import pytest
 
 from tests.test_kernel_resources import load
 
-KERNELS = {"paged_attn_kernel": ("kernels_paged_attn.hip", 12), "paged_attn_wide_kernel": ("kernels_paged_attn.hip", 4),
+KERNELS = {"paged_attn_kernel": ("kernels_paged_attn.hip", 16), "paged_attn_wide_kernel": ("kernels_paged_attn.hip", 4),
            "paged_attn_both_kernel": ("kernels_paged_attn.hip", 4), "paged_attn_f32_kernel": ("kernels_paged_attn.hip", 3),
-           "paged_combine_kernel": ("kernels_paged_attn.hip", 3), "paged_append_kernel": ("kernels_paged_cache.hip", 10),
+           "paged_combine_kernel": ("kernels_paged_attn.hip", 4), "paged_append_kernel": ("kernels_paged_cache.hip", 10),
            "page_copy_kernel": ("kernels_paged_cache.hip", 4)}
 
 
