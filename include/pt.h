@@ -225,7 +225,7 @@ typedef struct pt_paged_cache {
  *   row_start  int32 [n_seqs + 1], ascending from 0 on; rows from row_start[n_seqs] on are left as they are
  *   kv_len     int32 [n_seqs]
  *   pages      int32 [n_seqs, pages_stride]; entries beyond a sequence's last position are not read
- *   total_rows rows of the caller's buffers, an upper bound of row_start[n_seqs]
+ *   total_rows rows of the caller's buffers, an upper bound of row_start[n_seqs]; up to 2^23
  *   max_q_len, max_kv_len  upper bounds of n and kv_len (0: not known); tight ones make better launches, since
  *              the arrays are on the device.  max_kv_len <= pages_stride * page_size
  *   status     int32 on the device or NULL: bit 0 is raised when a page outside [0, n_pages) is met (page 0 is read in its
@@ -316,6 +316,7 @@ int pt_page_copy(const pt_paged_cache* cache, const int32_t* host_pairs, int32_t
  * to 2048 tokens and one less for each doubling of vocab from there on (lighter tokens come only of uniform = 0), and formed so that equal
  * inputs give equal tokens.  A row without any weight gives -1; where +infinity occurs, the tokens that have it share the
  * weight equally.
+ *   rows       up to 2^21
  *   vocab      1..2^24
  *   workspace  16-byte aligned device memory of pt_sample_bytes, or NULL where that is 0; needs no clearing
  * Errors: NULL_POINTER, INVALID_ARGUMENT, ARENA_TOO_SMALL. */

@@ -7,6 +7,13 @@
 
 #include "pt_serving.h"
 
+// Whether pt_sample and pt_sample_bytes take this many rows and tokens (a grid holds less than 2^32 threads, 1024 to a row).
+static int check_logits(int32_t rows, int32_t vocab) {
+  if (rows < 0 || rows > (1 << 21) || vocab < 1 || vocab > (1 << 24))
+    return pt_set_error(PT_ERR_INVALID_ARGUMENT, "rows must be in 0..2^21 and vocab in 1..2^24");
+  return PT_OK;
+}
+
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 static int check_cache(const pt_paged_cache* c) {
@@ -39,6 +46,7 @@ static int check_batch(const pt_paged_cache* c, const pt_paged_batch* b, bool ne
   if (!b) return pt_set_error(PT_ERR_NULL_POINTER, "batch is NULL");
   if (b->n_seqs < 0 || b->total_rows < 0 || b->pages_stride < 0 || b->max_q_len < 0 || b->max_kv_len < 0)
     return pt_set_error(PT_ERR_INVALID_ARGUMENT, "a size of the batch is negative");
+  if (b->total_rows > (1 << 23)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "total_rows = %d exceeds 2^23", b->total_rows);
   if (need_ptrs && b->n_seqs > 0 && b->total_rows > 0) {
     if (!b->row_start || !b->kv_len || (!b->pages && b->pages_stride > 0))
       return pt_set_error(PT_ERR_NULL_POINTER, "row_start, kv_len or pages is NULL");
@@ -238,7 +246,8 @@ extern "C" int pt_page_copy(const pt_paged_cache* cache, const int32_t* host_pai
 
 extern "C" int pt_sample_bytes(int32_t rows, int32_t vocab, size_t* bytes) {
   if (!bytes) return pt_set_error(PT_ERR_NULL_POINTER, "bytes is NULL");
-  if (rows < 0 || vocab < 1 || vocab > (1 << 24)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "rows must be >= 0 and vocab in 1..2^24");
+  const int rc = check_logits(rows, vocab);
+  if (rc) return rc;
   *bytes = rows == 0 ? 0 : pt_sample_workspace(rows, vocab);
   return PT_OK;
 }
@@ -246,7 +255,8 @@ extern "C" int pt_sample_bytes(int32_t rows, int32_t vocab, size_t* bytes) {
 extern "C" int pt_sample(const float* dev_logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* dev_uniform,
                          const float* dev_temperature, const int32_t* dev_top_k, const float* dev_top_p, const float* dev_min_p,
                          int32_t* dev_out, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  if (rows < 0 || vocab < 1 || vocab > (1 << 24)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "rows must be >= 0 and vocab in 1..2^24");
+  const int rc = check_logits(rows, vocab);
+  if (rc) return rc;
   if (rows == 0) return PT_OK;
   if (!dev_logits || !dev_uniform || !dev_out) return pt_set_error(PT_ERR_NULL_POINTER, "logits, uniform or out is NULL");
   if (row_stride < 0 || (rows > 1 && row_stride < vocab)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "row_stride is below vocab");

@@ -128,6 +128,20 @@ def test_batches_too_large_for_one_launch_are_refused():
     assert PB.lib().pt_paged_attention_bytes(c, batch(n_seqs=2 ** 31 - 1, total_rows=2 ** 31 - 1), 2 ** 10, C.byref(n)) == BAD
 
 
+def test_calls_whose_launches_would_hold_2_to_the_32_threads_are_refused():
+    n = C.c_size_t()
+    L = PB.lib()
+    assert append(b=batch(total_rows=(1 << 23) + 1)) == BAD and "2^23" in PB.pt_last_error()
+    assert attend(b=batch(total_rows=(1 << 23) + 1)) == BAD
+    # 2^20 rows of 16 heads on one KV head: 2^20 tiles of 16 rows; long ones are joined row by row
+    c = cache(dtype=PB.PT_F32, n_kv_heads=1, n_pages=100000, head_stride=0)
+    assert L.pt_paged_attention_bytes(c, batch(total_rows=1 << 20, n_seqs=1, pages_stride=512, max_kv_len=8192), 16, C.byref(n)) == 0
+    assert L.pt_paged_attention_bytes(c, batch(total_rows=1 << 20, n_seqs=1, pages_stride=1024, max_kv_len=16384), 16, C.byref(n)) == BAD
+    assert "too many tiles" in PB.pt_last_error()
+    assert L.pt_sample_bytes(1 << 21, 100, C.byref(n)) == 0 and L.pt_sample_bytes((1 << 21) + 1, 100, C.byref(n)) == BAD
+    assert L.pt_sample(0x1000, 100, (1 << 21) + 1, 100, 0x2000, None, None, None, None, 0x3000, None, 0, None) == BAD
+
+
 @pytest.mark.parametrize("args", [(2, 64, 1e4, 0, 1, 1, 2, 1, 1), (-1, 64, 1e4, 0, 1, 1, 2, 1, 1), (0, 0, 1e4, 0, 1, 1, 2, 1, 1), (0, 63, 1e4, 0, 1, 1, 2, 1, 1),
                                   (0, 258, 1e4, 0, 1, 1, 2, 1, 1), (0, 64, 0.0, 0, 1, 1, 2, 1, 1), (0, 64, float("nan"), 0, 1, 1, 2, 1, 1),
                                   (0, 64, float("inf"), 0, 1, 1, 2, 1, 1), (0, 64, 1e4, 3, 1, 1, 2, 1, 1), (0, 64, 1e4, 1, 0.0, 1, 2, 1, 1),
