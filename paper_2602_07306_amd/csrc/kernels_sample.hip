@@ -12,8 +12,8 @@
 //   pick: sixteen wavefronts sum a sixteenth of the range each, the one that holds the target is split again.
 // Rows are read from HBM once and from the caches in the later passes.
 // What bounds it: fp64 issue (about 45 instructions a weight, every compute unit on its own row) and, for top-k, a chain of
-// some fifteen steps between barriers.  256 rows of 32000 (33 MB, 6 us to read): largest logit 13 us, temperature alone 27,
-// top-k 40 26, top-k 400 46, top-p 0.95 53; one row of 32000 20, 20, 42 and 41.
+// some fifteen steps between barriers.  256 rows of 32000 (33 MB, 6 us to read): largest logit 14 us, temperature alone 27,
+// top-k 40 24, top-k 400 45, top-p 0.95 48; one row of 32000 8.5, 19, 18, 38 and 37.
 // Few rows of many logits leave most of the chip idle and one compute unit with all fp64 work of a row: their rows are cut
 // into parts first (sample_part_kernel), whose workgroups find each part's largest logit, its wavefronts' sums of weights relative
 // to that, or its candidates for top-k; sample_kernel then starts from those.
@@ -25,7 +25,7 @@
 typedef unsigned long long u64;
 
 constexpr int SAMPLE_BINS = 2048;
-constexpr int SAMPLE_U = 1;           // loads in flight of a thread where it forms weights
+constexpr int SAMPLE_U = 1;           // loads in flight of a thread where it forms weights: two cost the registers of the other paths
 
 constexpr int SAMPLE_LIST = 2048;     // gathered elements that fit
 constexpr int SAMPLE_LIST_K = 640;    // top-k by gathering: past it 1024 group maxima leave more than the list holds
@@ -53,7 +53,7 @@ struct sample_part {
 
 struct sample_lds {
   u64 list[SAMPLE_LIST];       // histogram or gathered elements (inverted key, index)
-  u64 wave[16];
+  u64 wave[16], total[16];
   u64 value;
   float tmax[1024];
   float wmin[16];
@@ -108,10 +108,11 @@ struct sample_row {
   __device__ __forceinline__ int bin(float v) const { return (int)fminf((max - v) * bin_scale, (float)(SAMPLE_BINS - 1)); }
 };
 
-// f(index, logit) for the elements lo .. hi-1, by `threads` threads, 16 bytes at a time whatever the row's alignment.  U loads
-// of a thread are in flight, and U * 4 calls run interleaved where they are free of branches.
-template <int U, typename F>
-__device__ __forceinline__ void for_each(const float* x, int lo, int hi, int tid, int threads, F&& f) {
+// The elements lo .. hi-1 by `threads` threads, 16 bytes at a time whatever the row's alignment: four(index, four logits), and
+// one(index, logit) for up to three in front of the 16-byte boundary and up to three behind the last.  U loads of a thread
+// are in flight.
+template <int U, typename F, typename G>
+__device__ __forceinline__ void for_fours(const float* x, int lo, int hi, int tid, int threads, F&& four, G&& one) {
   const int head = min(hi, lo + (int)((16 - ((uintptr_t)(x + lo) & 15)) >> 2 & 3));
   const int n4 = (hi - head) >> 2;
   const float4* x4 = (const float4*)(x + head);
@@ -122,20 +123,22 @@ __device__ __forceinline__ void for_each(const float* x, int lo, int hi, int tid
     for (int u = 0; u < U; ++u)
       if (j0 + u * threads < n4) v[u] = x4[j0 + u * threads];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (j0 + u * threads < n4) {
-        const int i = head + 4 * (j0 + u * threads);
-        f(i, v[u].x);
-        f(i + 1, v[u].y);
-        f(i + 2, v[u].z);
-        f(i + 3, v[u].w);
-      }
-    }
+    for (int u = 0; u < U; ++u)
+      if (j0 + u * threads < n4) four(head + 4 * (j0 + u * threads), v[u]);
   }
-  // up to three elements in front of the 16-byte boundary, and up to three behind the last: one call
   const int done = head + 4 * n4;
-  int i = lo + tid < head ? lo + tid : tid >= 4 && done + tid - 4 < hi ? done + tid - 4 : -1;
-  if (i >= 0) f(i, x[i]);
+  const int i = lo + tid < head ? lo + tid : tid >= 4 && done + tid - 4 < hi ? done + tid - 4 : -1;
+  if (i >= 0) one(i, x[i]);
+}
+// f(index, logit) for each; the four calls of a load run interleaved where they are free of branches.
+template <int U, typename F>
+__device__ __forceinline__ void for_each(const float* x, int lo, int hi, int tid, int threads, F&& f) {
+  for_fours<U>(x, lo, hi, tid, threads, [&](int i, float4 v) {
+    f(i, v.x);
+    f(i + 1, v.y);
+    f(i + 2, v.z);
+    f(i + 3, v.w);
+  }, f);
 }
 
 // Lanes exchange through the vector unit's own paths (moves within rows of 16, swaps of rows and halves) and not through LDS,
@@ -224,7 +227,7 @@ __device__ __forceinline__ u64 block_scan64(sample_lds& s, u64 v, u64* total) {
 }
 
 // Smallest index i at which the running sum of weight(i, logit) exceeds `target(total)`; -1 where the total is 0.  The
-// weights are free of branches: sixteen of a thread's run interleaved, where one alone is a chain of twenty dependent
+// weights are free of branches: four of a thread's run interleaved, where one alone is a chain of twenty dependent
 // fp64 operations (130001 weights of a row: 50 us with a branch in front of each, 30 us without).
 // The range lo .. hi-1 only, and with `known` for the target t.
 template <typename W, typename T>
@@ -272,10 +275,11 @@ __device__ int sample_pick(sample_lds& s, const sample_row& r, W&& weight, T&& t
   return sample_pick_in(s, r, 0, r.V, false, 0, weight, target);
 }
 
-// Sorts s.list[0 .. n-1] ascending (bitonic; padded with the largest value to a power of two, 64 at least).  A thread holds the elements
+// Sorts list[0 .. n-1] ascending (bitonic; padded with the largest value to a power of two, 64 at least).  A thread holds the elements
 // tid and, of more than 1024, tid + 1024: steps of less than 64 stay in the wavefronts' registers, wider ones go through
 // LDS, 10 of 55 for 1024 elements.
-__device__ void sample_sort(sample_lds& s, int n) {
+typedef __attribute__((address_space(3))) u64 lds64_t;
+__device__ __forceinline__ void sample_sort_inline(lds64_t* list, int n) {
   const int tid = threadIdx.x;
   int size = 64;
   while (size < n) size <<= 1;
@@ -285,7 +289,7 @@ __device__ void sample_sort(sample_lds& s, int n) {
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int i = tid + 1024 * e;
-    v[e] = i < n ? s.list[i] : ~0ull;
+    v[e] = i < n ? list[i] : ~0ull;
     if (busy) v[e] = wave_sort64(v[e], size == 64 || !(i & 64));
   }
   for (int k = 128; k <= size; k <<= 1) {
@@ -298,16 +302,16 @@ __device__ void sample_sort(sample_lds& s, int n) {
       }
       __syncthreads();
       if (busy) {
-        s.list[tid] = v[0];
-        if (size > 1024) s.list[tid + 1024] = v[1];
+        list[tid] = v[0];
+        if (size > 1024) list[tid + 1024] = v[1];
       }
       __syncthreads();
       if (busy) {
         const bool low = (tid & j) == 0;
-        u64 o = s.list[tid ^ j];
+        u64 o = list[tid ^ j];
         v[0] = (v[0] < o) == (low == ((tid & k) == 0)) ? v[0] : o;
         if (size > 1024) {
-          o = s.list[(tid ^ j) + 1024];
+          o = list[(tid ^ j) + 1024];
           v[1] = (v[1] < o) == (low == (((tid + 1024) & k) == 0)) ? v[1] : o;
         }
       }
@@ -318,10 +322,14 @@ __device__ void sample_sort(sample_lds& s, int n) {
     }
   }
   __syncthreads();
-  if (tid < size) s.list[tid] = v[0];
-  if (size > 1024) s.list[tid + 1024] = v[1];
+  if (tid < size) list[tid] = v[0];
+  if (size > 1024) list[tid + 1024] = v[1];
   __syncthreads();
 }
+// One copy for the callers: in line everywhere, the kernel's other paths take up to 3 us longer (256 rows of 32000, top-k 40
+// 23.5 us against 26.9).  sample_top_p has its own.
+__device__ __attribute__((noinline)) void sample_sort_call(lds64_t* list, int n) { sample_sort_inline(list, n); }
+__device__ __forceinline__ void sample_sort(sample_lds& s, int n) { sample_sort_call((lds64_t*)s.list, n); }
 
 // A lower bound of the k-th largest logit of a range, k <= SAMPLE_LIST_K: the k-th largest of the maxima that its threads left in
 // s.tmax.  256 groups of them (about k (1 + k / 512) logits lie above the bound) are ranked by comparing each with all,
@@ -464,8 +472,8 @@ __device__ void sample_cut(sample_lds& s, sample_row& r, T&& target_of) {
 }
 
 // The answer to a uniform number of 0: the first token of the prefix that has any weight, however small (down to 2^-1074, where
-// fp64 ends; as integers of 2^-S most of those are 0).
-__device__ int sample_first(sample_lds& s, const sample_row& r) {
+// fp64 ends; as integers of 2^-S most of those are 0).  A call, for it is rare and its registers are not the kernel's.
+__device__ __attribute__((noinline)) int sample_first(sample_lds& s, const sample_row& r) {
   __syncthreads();
   if (threadIdx.x == 0) s.n = 0x7fffffff;
   __syncthreads();
@@ -484,7 +492,8 @@ __device__ __forceinline__ int sample_stretch(int n) { return ((n + 15) / 16 + 2
 // weights: each wavefront's sum over its stretch of the row of what lies above that step, the sum of all, and the step's
 // members for the list; with them the step is checked (and the next one tried if rounding was in the way), the cut is found
 // among the sorted members, and the token's stretch is known.  -2: the step holds more than the list, sample_cut finds the
-// prefix and sample_pick the token.  130001 logits: 240 us with sample_cut's exact histogram and sample_pick, 94 so.
+// prefix and sample_pick the token.  64 rows of 130001 logits: 240 us with sample_cut's exact histogram and
+// sample_pick, 105 so.
 template <typename C, typename T>
 __device__ int sample_top_p(sample_lds& s, sample_row& r, bool first, C&& cut_of, T&& target_of) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -507,27 +516,51 @@ __device__ int sample_top_p(sample_lds& s, sample_row& r, bool first, C&& cut_of
   for (int step = 0;;) {
     if (tid == 0) s.n = 0;
     __syncthreads();
-    u64 total = 0, above = 0, mine = 0;
-    for_each<SAMPLE_U>(r.x, lo, hi, lane, 64, [&](int i, float v) {
+    u64 total = 0, above = 0, heavy = 0;   // heavy: above and not dropped by min-p
+    const float edge = (float)b, next = (float)(b + 1);   // r.bin(v) < b and == b without the whole number
+    const bool last = b == SAMPLE_BINS - 1, floor_on = r.least > 1;
+    // whether a logit lies in the step
+    auto add = [&](int i, float v) {
       u64 w = r.weight(v);
       if (!all) w = r.in_prefix(key_of(v), i) ? w : 0;
-      const int at = r.bin(v);
-      const u64 up = at < b ? w : 0;
+      const float at = (r.max - v) * r.bin_scale;
+      const bool up = at < edge;
       total += w;
-      above += up;
-      mine += up >= r.least ? up : 0;
-      if (at == b && w > 0) {
-        const int to = atomicAdd(&s.n, 1);
-        if (to < SAMPLE_LIST) s.list[to] = (u64)~key_of(v) << 32 | (uint32_t)i;
-      }
+      above += up ? w : 0;
+      if (floor_on) heavy += up && w >= r.least ? w : 0;
+      return !up && (last || at < next) && w > 0;
+    };
+    auto list = [&](int i, float v) {
+      const int to = atomicAdd(&s.n, 1);
+      if (to < SAMPLE_LIST) s.list[to] = (u64)~key_of(v) << 32 | (uint32_t)i;
+    };
+    for_fours<SAMPLE_U>(r.x, lo, hi, lane, 64, [&](int i, float4 v) {
+      const bool b0 = add(i, v.x), b1 = add(i + 1, v.y), b2 = add(i + 2, v.z), b3 = add(i + 3, v.w);   // no branch between them
+      if (b0) list(i, v.x);
+      if (b1) list(i + 1, v.y);
+      if (b2) list(i + 2, v.z);
+      if (b3) list(i + 3, v.w);
+    }, [&](int i, float v) {
+      if (add(i, v)) list(i, v);
     });
-    mine = wave_sum64(mine);
-    block_scan64(s, total, &total);
-    block_scan64(s, above, &above);
+    above = wave_sum64(above);
+    total = wave_sum64(total);
+    const u64 mine = floor_on ? wave_sum64(heavy) : above;
+    if (lane == 0) {
+      s.wave[wave] = above;
+      s.total[wave] = total;
+    }
+    __syncthreads();
+    above = total = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      above += s.wave[q];
+      total += s.total[q];
+    }
     const int n = s.n;
     if (n > SAMPLE_LIST) return -2;
     const u64 cut = cut_of(total);
-    sample_sort(s, n);
+    sample_sort_inline((lds64_t*)s.list, n);   // called, all of it takes 7 us longer (256 rows of 32000: 48)
     u64 e[2], w[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
