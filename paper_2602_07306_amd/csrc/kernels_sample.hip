@@ -488,9 +488,9 @@ __device__ __attribute__((noinline)) int sample_first(sample_lds& s, const sampl
 __device__ __forceinline__ int sample_stretch(int n) { return ((n + 15) / 16 + 255) / 256 * 256; }
 
 // Top-p (of what the prefix holds so far) and the token: with two passes over the row.  The first adds up fp32 weights by
-// steps of the logit, which tells the step that the cut falls into, give or take rounding.  The second forms the exact
-// weights: each wavefront's sum over its stretch of the row of what lies above that step, the sum of all, and the step's
-// members for the list; with them the step is checked (and the next one tried if rounding was in the way), the cut is found
+// steps of the logit, which tells the step that the cut falls into, give or take rounding (then its neighbour counts as part
+// of it).  The second forms the exact weights: each wavefront's sum over its stretch of the row of what lies above that
+// step, the sum of all, and the step's members for the list; with them the step is checked (and the next one tried), the cut is found
 // among the sorted members, and the token's stretch is known.  -2: the step holds more than the list, sample_cut finds the
 // prefix and sample_pick the token.  64 rows of 130001 logits: 240 us with sample_cut's exact histogram and
 // sample_pick, 105 so.
@@ -507,18 +507,26 @@ __device__ int sample_top_p(sample_lds& s, sample_row& r, bool first, C&& cut_of
     const float x = v == r.max ? r.top : r.infinite ? -INFINITY : v;
     float w = __builtin_amdgcn_exp2f(fmaxf((x - r.top) * c32, -126.0f));
     if (!all) w = r.in_prefix(key_of(v), i) ? w : 0.f;
-    atomicAdd(&s.list[r.bin(v)], (u64)(uint32_t)(w * 2147483648.0f));   // whole numbers: an LDS sum of floats takes 16 times as long
+    atomicAdd(&s.list[r.bin(v)], (u64)(uint32_t)fmaf(w, 2147483648.0f, 0.5f));   // whole numbers: an LDS sum of floats takes 16 times as long
   });
   __syncthreads();
   u64 need, before;
-  int b = max(sample_find_bin(s, s.list[2 * tid], s.list[2 * tid + 1], cut_of, &need, &before), 0);
+  const int found = sample_find_bin(s, s.list[2 * tid], s.list[2 * tid + 1], cut_of, &need, &before);
+  // The fp32 sums are off by some 2^-20 of what they hold.  Where the cut lies that near to an end of its step, the next step is
+  // listed too: another pass would cost 10 us, and one of a hundred rows would need it.
+  int first_bin = max(found, 0), last_bin = first_bin;
+  if (found >= 0) {
+    const u64 slack = (need >> 16) + r.V, mass = s.list[found];
+    if (need <= before + slack) first_bin = max(found - 1, 0);
+    if (need + slack >= before + mass) last_bin = min(found + 1, SAMPLE_BINS - 1);
+  }
   const int len = sample_stretch(r.V), lo = min(r.V, wave * len), hi = min(r.V, lo + len);
   for (int step = 0;;) {
     if (tid == 0) s.n = 0;
     __syncthreads();
     u64 total = 0, above = 0, heavy = 0;   // heavy: above and not dropped by min-p
-    const float edge = (float)b, next = (float)(b + 1);   // r.bin(v) < b and == b without the whole number
-    const bool last = b == SAMPLE_BINS - 1, floor_on = r.least > 1;
+    const float edge = (float)first_bin, next = (float)(last_bin + 1);   // r.bin(v) < first_bin and <= last_bin without the whole number
+    const bool last = last_bin == SAMPLE_BINS - 1, floor_on = r.least > 1;
     // whether a logit lies in the step
     auto add = [&](int i, float v) {
       u64 w = r.weight(v);
@@ -570,9 +578,9 @@ __device__ int sample_top_p(sample_lds& s, sample_row& r, bool first, C&& cut_of
     }
     u64 inside;
     const u64 c = block_scan64(s, w[0] + w[1], &inside), start = above + c - w[0] - w[1];
-    // the cut lies above this step, or below it: never both ways, for the sums are exact
-    if (cut <= above && b > 0 && step <= 0) { step = -1; --b; __syncthreads(); continue; }
-    if (cut > above + inside && b < SAMPLE_BINS - 1 && step >= 0) { step = 1; ++b; __syncthreads(); continue; }
+    // the cut lies above these steps, or below them: never both ways, for the sums are exact
+    if (cut <= above && first_bin > 0 && step <= 0) { step = -1; last_bin = --first_bin; __syncthreads(); continue; }
+    if (cut > above + inside && last_bin < SAMPLE_BINS - 1 && step >= 0) { step = 1; first_bin = ++last_bin; __syncthreads(); continue; }
     __syncthreads();
     if (lane == 0) s.wave[wave] = mine;
     if (start < cut && start + w[0] + w[1] >= cut) s.value = start + w[0] >= cut ? e[0] : e[1];
