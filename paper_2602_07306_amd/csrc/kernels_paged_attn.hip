@@ -220,7 +220,7 @@ __device__ __forceinline__ void paged_merge(const pt_paged_attn_args& a, const p
 // (16 lanes read a 4 x 16 block and receive its columns).
 // MFMA contraction order of the second product: lane group g holds, of 32 keys, 4g..4g+3 of the first and of the second
 // 16 - what the S^T result leaves in its registers, and what two transposing reads deliver.
-// What bounds it is HBM: 64 sequences of 128 to 8192 keys on 16 KV heads of 128, 2.19 GB, 378 us = 5.8 TB/s where a streaming read
+// What bounds it is HBM: 64 sequences of 128 to 8192 keys on 16 KV heads of 128, 2.19 GB, 381 us = 5.7 TB/s where a streaming read
 // reaches 6.0 to 6.2; tiles of 32 keys instead of 64 there 399.  One workgroup holds 128 KB of tiles at hd = 128.
 // NQ: blocks of 16 packed rows.  FULL: hd == HD; otherwise the rest of the LDS rows is zeroed once and never loaded.
 // ------------------------------------------------------------------------------------------------

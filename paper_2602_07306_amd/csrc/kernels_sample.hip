@@ -13,7 +13,7 @@
 // Rows are read from HBM once and from the caches in the later passes.
 // What bounds it: fp64 issue (about 45 instructions a weight, every compute unit on its own row) and, for top-k, a chain of
 // some fifteen steps between barriers.  256 rows of 32000 (33 MB, 6 us to read): largest logit 14 us, temperature alone 27,
-// top-k 40 24, top-k 400 45, top-p 0.95 48; one row of 32000 8.5, 19, 18, 38 and 37.
+// top-k 40 24, top-k 400 45, top-p 0.95 47; one row of 32000 8.5, 19, 18, 38 and 37.
 // Few rows of many logits leave most of the chip idle and one compute unit with all fp64 work of a row: their rows are cut
 // into parts first (sample_part_kernel), whose workgroups find each part's largest logit, its wavefronts' sums of weights relative
 // to that, or its candidates for top-k; sample_kernel then starts from those.
@@ -568,7 +568,7 @@ __device__ int sample_top_p(sample_lds& s, sample_row& r, bool first, C&& cut_of
     const int n = s.n;
     if (n > SAMPLE_LIST) return -2;
     const u64 cut = cut_of(total);
-    sample_sort_inline((lds64_t*)s.list, n);   // called, all of it takes 7 us longer (256 rows of 32000: 48)
+    sample_sort_inline((lds64_t*)s.list, n);   // called, all of it takes 7 us longer (256 rows of 32000: 47)
     u64 e[2], w[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {

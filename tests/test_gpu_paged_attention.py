@@ -160,6 +160,15 @@ def test_long_sequences_cut_into_ranges(H, Hkv, hd, dtype):
     assert torch.equal(a, p.run())       # the same from call to call
 
 
+@pytest.mark.parametrize("H,hd,dtype", [(1, 128, "bf16"), (20, 128, "bf16"), (2, 96, "bf16"), (1, 64, "bf16"), (3, 256, "bf16"), (2, 64, "fp32")])
+def test_very_long_sequences(H, hd, dtype):
+    # ranges of more than 1024 keys, more than 50 of them, beside sequences of one range and of two
+    p = Problem(H, 1, hd, dtype, 64, [(1, 70001), (1, 30), (1, 1025), (0, 0), (1, 1300)], seed=H + hd, layers=1, layer=0)
+    out = p.run()
+    p.check(out)
+    assert torch.equal(p.run(), out)
+
+
 def test_bounds_need_not_be_tight():
     p = Problem(4, 2, 64, "bf16", 16, MIXED, seed=9)
     tight = p.run()
