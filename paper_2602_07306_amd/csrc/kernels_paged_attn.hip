@@ -239,7 +239,7 @@ struct paged_geom {
 // it positive); m0, the LDS address, is set once for four.  Inline assembly because the compiler takes any LDS read to
 // depend on such a load of its own and waits for all of them in front of it, that is for the next tile in front of this
 // one's first product.  There are no result registers; every wait for these loads is written out.
-constexpr int LDS_BIAS = 3072;
+constexpr int LDS_BIAS = 3 * 1024;
 template <int N, bool FULL>
 __device__ __forceinline__ void load_keys_to_lds(uint32_t lds, const char* base, const uint32_t (&off)[N], const bool (&on)[N]) {
   if constexpr (FULL && N == 2) {
@@ -249,8 +249,8 @@ __device__ __forceinline__ void load_keys_to_lds(uint32_t lds, const char* base,
 #pragma unroll
     for (int i = 0; i < N; i += 4)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-                   "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
-                   ::"s"(lds + i * 1024), "v"(off[i]), "v"(off[i + 1]), "v"(off[i + 2]), "v"(off[i + 3]), "s"(base) : "memory", "m0");
+                   "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:%6"
+                   ::"s"(lds + i * 1024), "v"(off[i]), "v"(off[i + 1]), "v"(off[i + 2]), "v"(off[i + 3]), "s"(base), "n"(LDS_BIAS) : "memory", "m0");
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
