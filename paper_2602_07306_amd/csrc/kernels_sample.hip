@@ -15,8 +15,9 @@
 // some fifteen steps between barriers.  256 rows of 32000 (33 MB, 6 us to read): largest logit 14 us, temperature alone 27,
 // top-k 40 24, top-k 400 45, top-p 0.95 47; one row of 32000 8.5, 19, 18, 38 and 37.
 // Few rows of many logits leave most of the chip idle and one compute unit with all fp64 work of a row: their rows are cut
-// into parts first (sample_part_kernel), whose workgroups find each part's largest logit, its wavefronts' sums of weights relative
-// to that, or its candidates for top-k; sample_kernel then starts from those.
+// into parts first.  sample_part_kernel finds each part's largest logit and its candidates for top-k, sample_sum_kernel each
+// wavefront's sum of weights relative to the row's largest; sample_kernel then starts from those.  The sums are the integers
+// that a row in one piece is summed by, so a row's token does not depend on how many rows the call has.
 #include <algorithm>
 
 #include "pt_device.h"
@@ -47,7 +48,7 @@ constexpr int SAMPLE_PART_LIST = 512; // candidates of a part that fit
 struct sample_part {
   float max, min;            // largest logit, smallest finite one
   int n, pad;                // candidates found (more than fit: none are there); -1: not asked for
-  u64 sum[16];               // weights of each wavefront's stretch, relative to max
+  u64 sum[16];               // weights of each wavefront's stretch, relative to the row's largest logit
   u64 list[SAMPLE_PART_LIST];
 };
 
@@ -654,13 +655,12 @@ __device__ __forceinline__ sample_row sample_load_row(const pt_sample_args& a, i
 // One part of a row: a.part_len logits from part * a.part_len on.
 __global__ void __launch_bounds__(1024) sample_part_kernel(const pt_sample_args a) {
   __shared__ sample_lds s;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x;
   const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
   sample_part* const to = (sample_part*)a.ws + blockIdx.x;
   const float temperature = a.temperature ? a.temperature[row] : 1.0f;
   const int top_k = a.top_k ? a.top_k[row] : 0;
-  const float top_p = a.top_p ? a.top_p[row] : 1.0f, min_p = a.min_p ? a.min_p[row] : 0.0f;
-  sample_row r = sample_load_row(a, row, temperature, min_p);
+  const sample_row r = sample_load_row(a, row, temperature, 0.0f);
   const int lo = min(r.V, part * a.part_len), hi = min(r.V, lo + a.part_len);
   float mx, mn;
   sample_extremes(s, r.x, lo, hi, &mx, &mn);
@@ -670,76 +670,63 @@ __global__ void __launch_bounds__(1024) sample_part_kernel(const pt_sample_args 
     to->n = -1;
   }
   if (mx == -INFINITY || !(temperature > 0.0f)) return;
-  const bool k_on = top_k > 0 && top_k < r.V;
-  if (k_on && top_k <= SAMPLE_PART_K) {
+  if (top_k > 0 && top_k < r.V && top_k <= SAMPLE_PART_K) {
     const float bound = sample_bound(s, top_k);
     const int n = sample_gather(s, r, lo, hi, [&](int, float v) { return v >= bound && v > -INFINITY; });
     if (tid == 0) to->n = n;
     if (n <= SAMPLE_PART_LIST && tid < n) to->list[tid] = s.list[tid];
-  } else if (!k_on && !(top_p < 1.0f) && !(min_p > 0.0f)) {
-    r.set_max(mx);
-    const int len = sample_stretch(hi - lo), from = min(hi, lo + wave * len);
-    u64 sum = 0;
-    for_each<SAMPLE_U>(r.x, from, min(hi, from + len), lane, 64, [&](int, float v) { sum += r.weight(v); });
-    sum = wave_sum64(sum);
-    if (lane == 0) to->sum[wave] = sum;
   }
 }
 
-// A row of temperature alone from its parts' sums: which stretch the target falls into, and the token inside it.  The
-// parts' sums are relative to their own largest logit; their factors and the running sum over stretches are fp64, formed
-// in one order.
-__device__ int sample_from_sums(sample_lds& s, sample_row& r, const sample_part* parts, const pt_sample_args& a, double u) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int n = a.parts * 16;
-  __syncthreads();
-  double* const run = (double*)s.list;   // [n + 1] sums in front of a stretch
-  if (tid < 64) {
-    double v[4], before = 0.0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = lane * 4 + j;
-      v[j] = 0.0;
-      if (i < n) {
-        const sample_part& p = parts[i >> 4];
-        if (p.max == r.max) v[j] = (double)p.sum[i & 15];
-        else if (!r.infinite && p.max > -INFINITY) v[j] = (double)p.sum[i & 15] * r.power(p.max);
-      }
-    }
-    const double own = v[0] + v[1] + v[2] + v[3];
-    before = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double up = __shfl_up(before, o, 64);
-      if (lane >= o) before += up;
-    }
-    before -= own;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (lane * 4 + j <= n) run[lane * 4 + j] = before;
-      before += v[j];
-    }
-    if (lane == 63 && n == 256) run[n] = before;
+// Whether a row has no filter: its parts' sums serve it.
+__device__ __forceinline__ bool sample_no_filter(int top_k, float top_p, float min_p, int vocab) {
+  return !(top_k > 0 && top_k < vocab) && !(top_p < 1.0f) && !(min_p > 0.0f);
+}
+// Largest logit of a row from its parts (every lane of a wavefront must call this).
+__device__ __forceinline__ float sample_parts_max(const sample_part* parts, int n) {
+  const int lane = threadIdx.x & 63;
+  return wave_max(lane < n ? parts[lane].max : -INFINITY);
+}
+
+// Sums of weights of a part's stretches, of rows without a filter.
+__global__ void __launch_bounds__(1024) sample_sum_kernel(const pt_sample_args a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+  const float temperature = a.temperature ? a.temperature[row] : 1.0f;
+  if (!(temperature > 0.0f) || !sample_no_filter(a.top_k ? a.top_k[row] : 0, a.top_p ? a.top_p[row] : 1.0f, a.min_p ? a.min_p[row] : 0.0f, a.vocab)) return;
+  sample_part* const parts = (sample_part*)a.ws + row * a.parts;
+  sample_row r = sample_load_row(a, row, temperature, 0.0f);
+  r.set_max(sample_parts_max(parts, a.parts));
+  if (r.max == -INFINITY) return;
+  const int lo = min(r.V, part * a.part_len), hi = min(r.V, lo + a.part_len);
+  const int len = sample_stretch(hi - lo), from = min(hi, lo + wave * len);
+  u64 sum = 0;
+  for_each<SAMPLE_U>(r.x, from, min(hi, from + len), lane, 64, [&](int, float v) { sum += r.weight(v); });
+  sum = wave_sum64(sum);
+  if (lane == 0) parts[part].sum[wave] = sum;
+}
+
+// A row without a filter from its parts' sums: which stretch the target falls into, and the token inside it.
+template <typename T>
+__device__ int sample_from_sums(sample_lds& s, const sample_row& r, const sample_part* parts, const pt_sample_args& a, T&& target_of) {
+  const int tid = threadIdx.x;
+  const u64 own = tid < a.parts * 16 ? parts[tid >> 4].sum[tid & 15] : 0;
+  u64 total;
+  const u64 c = block_scan64(s, own, &total), t = target_of(total);
+  if (c - own <= t && c > t) {   // one thread: t < total
+    s.found = tid;
+    s.value = c - own;
   }
-  if (tid == 0) s.n = -1;
   __syncthreads();
-  const double t = u * run[n];
-  if (tid < n && run[tid] <= t && parts[tid >> 4].sum[tid & 15] > 0 && parts[tid >> 4].max > -INFINITY && !(r.infinite && parts[tid >> 4].max != r.max))
-    atomicMax(&s.n, tid);   // the last stretch whose start the target reaches
+  const int at = s.found;
+  const u64 before = s.value;
   __syncthreads();
-  const int at = s.n, part = at >> 4;
-  const double start = run[at];
-  const u64 sum = parts[part].sum[at & 15];
-  const double scale = parts[part].max == r.max ? 1.0 : r.power(parts[part].max);
-  __syncthreads();
-  const int p0 = min(r.V, part * a.part_len), p1 = min(r.V, p0 + a.part_len), len = sample_stretch(p1 - p0);
+  const int p0 = min(r.V, (at >> 4) * a.part_len), p1 = min(r.V, p0 + a.part_len), len = sample_stretch(p1 - p0);
   const int lo = min(p1, p0 + (at & 15) * len), hi = min(p1, lo + len);
-  r.set_max(parts[part].max);
-  const u64 local = (u64)fmax((t - start) / scale, 0.0);
-  return sample_pick_in(s, r, lo, hi, true, min(local, sum - 1), [&](int, float v) { return r.weight(v); }, [](u64 x) { return x; });
+  return sample_pick_in(s, r, lo, hi, true, t - before, [&](int, float v) { return r.weight(v); }, [](u64 x) { return x; });
 }
 
-// PARTS: sample_part_kernel ran before.
+// PARTS: sample_part_kernel and sample_sum_kernel ran before.
 template <bool PARTS>
 __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
   __shared__ sample_lds s;
@@ -753,10 +740,8 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
   const sample_part* const parts = PARTS ? (const sample_part*)a.ws + row * a.parts : nullptr;
   float mx, mn;
   if constexpr (PARTS) {
-    mx = lane < a.parts ? parts[lane].max : -INFINITY;
-    mn = lane < a.parts ? parts[lane].min : INFINITY;
-    mx = wave_max(mx);
-    mn = -wave_max(-mn);
+    mx = sample_parts_max(parts, a.parts);
+    mn = -wave_max(lane < a.parts ? -parts[lane].min : -INFINITY);
   } else {
     sample_extremes(s, r.x, 0, r.V, &mx, &mn);
   }
@@ -787,8 +772,8 @@ __global__ void __launch_bounds__(1024) sample_kernel(const pt_sample_args a) {
   auto target = [&](u64 total) { return min((u64)(u * (double)total), total - 1); };
   auto cut_mass = [&](u64 total) { return max((u64)1, min((u64)ceil(fmax((double)top_p, 0.0) * (double)total), total)); };
   if constexpr (PARTS) {
-    if (!k_on && !p_on && !(min_p > 0.0f) && u > 0.0) {
-      const int token = sample_from_sums(s, r, parts, a, u);
+    if (sample_no_filter(top_k, top_p, min_p, r.V) && u > 0.0) {
+      const int token = sample_from_sums(s, r, parts, a, target);
       if (tid == 0) a.out[row] = token;
       return;
     }
@@ -981,6 +966,7 @@ int pt_launch_sample(const pt_sample_args& args, hipStream_t s) {
   a.part_len = ((a.vocab + a.parts - 1) / a.parts + 1023) / 1024 * 1024;
   if (a.parts > 1) {
     hipLaunchKernelGGL(sample_part_kernel, dim3((unsigned)(a.rows * a.parts)), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL(sample_sum_kernel, dim3((unsigned)(a.rows * a.parts)), dim3(1024), 0, s, a);
     hipLaunchKernelGGL(sample_kernel<true>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
   } else {
     hipLaunchKernelGGL(sample_kernel<false>, dim3((unsigned)a.rows), dim3(1024), 0, s, a);
