@@ -1080,14 +1080,14 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
   if (t0 > 0) paged_ranges(t0 * Hkv, keys, dtype == PT_F32 ? 256 : 1024, 8192, &p->cut[0]);
   // Many rows: by the number of tiles that the rows make up, not its bound.
   if (t1 > 0) paged_ranges((b.total_rows * G / PA_WIDE_ROWS + 1) * Hkv, keys, 256, keys, &p->cut[1]);
-  // workgroups of the two launches: a grid holds less than 2^32 threads
+  // workgroups of the two launches: a grid holds less than 2^32 threads, where both kinds run in one each in whole stretches
   int64_t runs = 0, joins = 0;
   for (int c = 0; c < 2; ++c) {
     const int64_t tiles = (c ? t1 : t0) * Hkv;
-    runs += tiles * p->cut[c].n_splits;
+    runs += (tiles * p->cut[c].n_splits + PA_DEAL - 1) / PA_DEAL * PA_DEAL;
     if (p->cut[c].n_splits > 1) joins += tiles * p->cut[c].tile_rows;
   }
-  if (std::max(runs, joins) >= (1 << 24) - 64) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
+  if (std::max(runs, joins) >= 1 << 24) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
   const int32_t splits = std::max(p->cut[0].n_splits, p->cut[1].n_splits);
   if (splits > 1) {
     const size_t parts = (size_t)splits * b.total_rows * H;
