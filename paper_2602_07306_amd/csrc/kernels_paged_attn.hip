@@ -163,16 +163,33 @@ __device__ __forceinline__ bool paged_odd_values(const pt_paged_attn_args& a, co
   return __any(odd);
 }
 
+// A class's partials.
+template <bool WIDE>
+struct paged_parts {
+  float* o;
+  float2* ml;
+  __device__ __forceinline__ explicit paged_parts(const pt_paged_attn_args& a) {
+    o = a.part + (WIDE ? pt_paged_part_size(a.cut[0].n_splits, a.part_rows[0], a.H, a.hd) : 0);
+    ml = (float2*)(o + (int64_t)a.cut[WIDE].n_splits * a.part_rows[WIDE] * a.H * a.hd);
+  }
+  // that of (range, new row i of the tile's sequence, head), counted in heads of rows
+  static __device__ __forceinline__ int64_t at(const pt_paged_attn_args& a, const paged_tile& t, int split, int i, int head) {
+    const int64_t row = WIDE || a.seq_rows == 0 ? t.sq.first + i : (int64_t)t.seq * a.seq_rows + i;
+    return ((int64_t)split * a.part_rows[WIDE] + row) * a.H + head;
+  }
+};
+
 // Result of one row over one range: the output itself, or a partial for the combine.
-template <typename T>
-__device__ __forceinline__ void paged_store_row(const pt_paged_attn_args& a, const paged_tile& t, int split, int row, int head, int lim, float m, float l, float o, int e) {
+template <typename T, bool WIDE>
+__device__ __forceinline__ void paged_store_row(const pt_paged_attn_args& a, const paged_tile& t, int split, int i, int head, int lim, float m, float l, float o, int e) {
   if (t.nsplit == 1) {
     // sees nothing: zero; sees only scores of -infinity: 0 / 0
-    elem<T>::st((T*)a.o + row * a.o_rs + head * a.o_hs + e, lim <= 0 ? 0.f : o / l);
+    elem<T>::st((T*)a.o + (t.sq.first + i) * a.o_rs + head * a.o_hs + e, lim <= 0 ? 0.f : o / l);
   } else {
-    const int64_t at = ((int64_t)split * a.b.total_rows + row) * a.H + head;
-    a.part_o[at * a.hd + e] = o;
-    if (e == 0) a.part_ml[at] = make_float2(m, l);
+    const paged_parts<WIDE> parts(a);
+    const int64_t at = parts.at(a, t, split, i, head);
+    parts.o[at * a.hd + e] = o;
+    if (e == 0) parts.ml[at] = make_float2(m, l);
   }
 }
 
@@ -209,7 +226,7 @@ __device__ __forceinline__ void paged_merge(const pt_paged_attn_args& a, const p
     }
 #pragma unroll
     for (int j = 0; j < PER; ++j)
-      if (lane + 64 * j < a.hd) paged_store_row<T>(a, t, split, row, head, lim, m, l, o[j], lane + 64 * j);
+      if (lane + 64 * j < a.hd) paged_store_row<T, false>(a, t, split, i, head, lim, m, l, o[j], lane + 64 * j);
   }
 }
 
@@ -805,7 +822,6 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
                                            max(k0, lim_first), min(k1, k0 + own * UK + UK)))
       again = 0;
     if (real && !(again >> l16 & 1)) {   // the others' queries are read once more, and the output may lie over them
-      const int64_t at = ((int64_t)split * a.b.total_rows + row) * a.H + head;
       if (t.nsplit == 1) {
         const float inv = see <= 0 ? 0.f : 1.0f / l;
         bf16_t* o = (bf16_t*)a.o + row * a.o_rs + head * a.o_hs + 4 * g;
@@ -818,10 +834,12 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
             *(uint2*)(o + hb * 16) = w;
           }
       } else {
+        const paged_parts<true> parts(a);
+        const int64_t at = parts.at(a, t, split, i, head);
 #pragma unroll
         for (int hb = 0; hb < HB; ++hb)
-          if (FULL || hb * 16 + 4 * g < a.hd) *(f32x4_t*)(a.part_o + at * a.hd + hb * 16 + 4 * g) = acc[n][hb];
-        if (g == 0) a.part_ml[at] = make_float2(m, l);
+          if (FULL || hb * 16 + 4 * g < a.hd) *(f32x4_t*)(parts.o + at * a.hd + hb * 16 + 4 * g) = acc[n][hb];
+        if (g == 0) parts.ml[at] = make_float2(m, l);
       }
     }
     for (int j = 0; j < 16; ++j)
@@ -834,7 +852,7 @@ __device__ __forceinline__ void paged_many_rows(const pt_paged_attn_args& a, int
                                 a.b.pages + t.seq * a.b.pages_stride, k0, min(k1, limj), &mj, &lj, oj);
 #pragma unroll
         for (int e = 0; e < HD / 64; ++e)
-          if (lane + 64 * e < a.hd) paged_store_row<bf16_t>(a, t, split, rowj, hj, limj, mj, lj, oj[e], lane + 64 * e);
+          if (lane + 64 * e < a.hd) paged_store_row<bf16_t, true>(a, t, split, ij, hj, limj, mj, lj, oj[e], lane + 64 * e);
       }
   }
 #endif
@@ -999,11 +1017,12 @@ __device__ __forceinline__ void paged_combine(const pt_paged_attn_args& a, int b
   if (!paged_find_tile<WIDE>(a, rest / parts, &t) || t.nsplit == 1) return;
   const int r = rest % parts * (4 / SHARE) + (SHARE == 4 ? 0 : wave);
   if (r >= t.nrows) return;                         // SHARE = 4: all four wavefronts alike
-  const int64_t step = (int64_t)a.b.total_rows * a.H;
+  const int64_t step = (int64_t)a.part_rows[WIDE] * a.H;
   const int i = (t.row0 + r) / G, head = kvh * G + (t.row0 + r) - i * G, row = t.sq.first + i;
-  const int64_t at = (int64_t)row * a.H + head;
+  const paged_parts<WIDE> from(a);
+  const int64_t at = from.at(a, t, 0, i, head);
   float2 ml = make_float2(-INFINITY, 0.f);
-  if (lane < t.nsplit) ml = a.part_ml[lane * step + at];
+  if (lane < t.nsplit) ml = from.ml[lane * step + at];
   const float m = wave_max(ml.x);
   const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
   const float l = wave_sum(f * ml.y);
@@ -1017,7 +1036,7 @@ __device__ __forceinline__ void paged_combine(const pt_paged_attn_args& a, int b
       const float fs = __shfl(f, min(s + u, 63), 64);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (s + u < s1 && lane + 64 * j < a.hd) o[j] += fs * a.part_o[((s + u) * step + at) * a.hd + lane + 64 * j];
+        if (s + u < s1 && lane + 64 * j < a.hd) o[j] += fs * from.o[((s + u) * step + at) * a.hd + lane + 64 * j];
     }
   }
   if constexpr (SHARE == 4) {
@@ -1088,12 +1107,15 @@ int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const 
     if (p->cut[c].n_splits > 1) joins += tiles * p->cut[c].tile_rows;
   }
   if (std::max(runs, joins) >= 1 << 24) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the batch has too many tiles of rows for one call");
-  const int32_t splits = std::max(p->cut[0].n_splits, p->cut[1].n_splits);
-  if (splits > 1) {
-    const size_t parts = (size_t)splits * b.total_rows * H;
-    p->off_ml = (parts * hd * 4 + 15) / 16 * 16;
-    p->bytes = p->off_ml + parts * 8;
+  // Partials of each class that is cut.  Beside chunks, the rows of sequences of few rows are a small part of all: they are counted
+  // by sequence.  One decode step beside a chunk of 2048 over 16384 keys, 64 heads on 8 KV heads of 128: 4.3 MB, by rows of
+  // the batch 2.2 GB.
+  p->part_rows[0] = p->part_rows[1] = b.total_rows;
+  if (wide && t0 > 0 && b.n_seqs * (p->few / G) < b.total_rows) {
+    p->seq_rows = (int32_t)(p->few / G);
+    p->part_rows[0] = b.n_seqs * p->seq_rows;
   }
+  for (int c = 0; c < 2; ++c) p->bytes += (size_t)pt_paged_part_size(p->cut[c].n_splits, p->part_rows[c], H, hd) * sizeof(float);
   return PT_OK;
 }
 

@@ -203,8 +203,8 @@ extern "C" int pt_paged_attention(const pt_paged_cache* cache, int32_t layer, co
   a.kc = layer_of(cache->k, cache, layer);
   a.vc = layer_of(cache->v, cache, layer);
   a.page_stride = cache->page_stride; a.head_stride = cache->head_stride; a.token_stride = cache->token_stride;
-  a.part_o = (float*)workspace;
-  a.part_ml = (float2*)((char*)workspace + plan.off_ml);
+  a.part = (float*)workspace;
+  a.part_rows[0] = plan.part_rows[0]; a.part_rows[1] = plan.part_rows[1]; a.seq_rows = plan.seq_rows;
   a.scale_log2 = scale == 0.0f ? 1.0f : (float)(fabs((double)scale) * 1.4426950408889634);
   a.q_sign = scale == 0.0f ? 0.0f : scale < 0.0f ? -1.0f : 1.0f;
   a.causal = causal != 0;

@@ -44,8 +44,11 @@ struct pt_paged_attn_args {
   const void* vc;
   int64_t q_rs, q_hs, o_rs, o_hs;
   int64_t page_stride, head_stride, token_stride;
-  float* part_o;     // [n_splits][total_rows][H][hd] unscaled sums
-  float2* part_ml;   // [n_splits][total_rows][H] (reference of the exponents in binary orders, sum)
+  // What the ranges leave to be joined, class by class (of those that are cut): [cut[c].n_splits][part_rows[c]][H][hd] unscaled sums,
+  // then [cut[c].n_splits][part_rows[c]][H] (reference of the exponents in binary orders, sum).
+  float* part;
+  int32_t part_rows[2];
+  int32_t seq_rows;  // > 0: new row i of sequence b is row b * seq_rows + i of class 0's; else rows are those of the batch
   float scale_log2;  // |scale| * log2 e, or 1 where the scale is 0
   float q_sign;      // what the queries are multiplied with for that: 1, -1 or 0
   int32_t causal, H, Hkv, hd;
@@ -58,8 +61,14 @@ struct pt_paged_attn_args {
 struct pt_paged_plan {
   int32_t few;
   pt_paged_cut cut[2];
-  size_t off_ml, bytes;   // workspace: part_o first
+  int32_t part_rows[2], seq_rows;
+  size_t bytes;   // workspace
 };
+
+// Elements of the partials of a class that is cut, a multiple of 16 bytes.
+__host__ __device__ inline int64_t pt_paged_part_size(int32_t n_splits, int32_t rows, int32_t H, int32_t hd) {
+  return n_splits > 1 ? ((int64_t)n_splits * rows * H * (hd + 2) + 3) / 4 * 4 : 0;
+}
 
 int pt_launch_paged_append(const pt_append_args& a, const pt_rope* rope, int32_t dtype, hipStream_t s);
 int pt_plan_paged_attn(int32_t dtype, int32_t hd, int32_t H, int32_t Hkv, const pt_paged_rows& b, pt_paged_plan* p);

@@ -24,3 +24,22 @@ def test_workgroups_of_both_kinds_in_one_launch_are_counted_in_whole_stretches()
     assert few % 64 == 1
     assert attention_bytes(c, b(few), 16)[0] == BAD and "too many tiles" in PB.pt_last_error()
     assert attention_bytes(c, b(few - 1), 16) == (0, 0)
+
+
+def test_workspaces_hold_the_partials_of_rows_that_are_cut_and_no_others():
+    """A partial is head_dim + 2 fp32 values per head of a row and range, 64 ranges at most.  Sequences of few rows: 16 packed
+    rows each, of as many heads as share a KV head.  Chunks of more tiles than fill the chip are not cut."""
+    c = lambda **kw: cache(n_kv_heads=8, head_dim=128, page_size=32, n_pages=100000, token_stride=128, head_stride=4096, page_stride=32768, layer_stride=0, **kw)
+    part, group = 4 * 130 * 64, 8                # bytes of a row's partials in one range, 64 heads
+    few = lambda n: n * (16 // group) * part * 64 + 32
+    for seqs, rows, longest in ((2, 2049, 16384), (2, 2049, 131072), (8, 8199, 131072), (40, 36 + 4 * 400, 2048)):
+        rc, n = attention_bytes(c(), batch(n_seqs=seqs, total_rows=rows, pages_stride=8192, max_q_len=rows - seqs + 1, max_kv_len=longest), 64)
+        assert rc == 0 and 0 < n <= few(seqs), (seqs, rows, longest, n)
+    assert attention_bytes(c(), batch(n_seqs=2, total_rows=4096, pages_stride=8192, max_q_len=2048, max_kv_len=16384), 64)[1] <= few(2)
+    assert attention_bytes(c(), batch(n_seqs=1, total_rows=2048, pages_stride=8192, max_q_len=2048, max_kv_len=131072), 64) == (0, 0)
+    # one chunk of a few tiles: its ranges make up 512 workgroups, a range for each of them and one more round
+    rc, n = attention_bytes(c(), batch(n_seqs=1, total_rows=300, pages_stride=8192, max_q_len=300, max_kv_len=131072), 64)
+    assert rc == 0 and 0 < n <= (512 + 160) * 128 * 4 * 130 + 32
+    # decode steps alone: by rows, as many as there are
+    rc, n = attention_bytes(c(), batch(n_seqs=16, total_rows=16, pages_stride=8192, max_q_len=1, max_kv_len=131072), 64)
+    assert rc == 0 and n == 16 * 16 * part
