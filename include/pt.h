@@ -231,7 +231,7 @@ typedef struct pt_paged_cache {
  *   status     int32 on the device or NULL: bit 0 is raised when a page outside [0, n_pages) is met (page 0 is read in its
  *              place, nothing is written to it), bit 1 when row_start, kv_len or their bounds contradict each other
  *              (they are clamped).  The outputs of those sequences are meaningless; nothing outside the buffers is touched.
- * All pointers are device pointers. */
+ * All pointers are device pointers.  With n_seqs or total_rows 0 there is nothing to do, and they and the rows' buffers may be NULL. */
 typedef struct pt_paged_batch {
   const int32_t* row_start;
   const int32_t* kv_len;

@@ -41,13 +41,16 @@ static int check_layer(const pt_paged_cache* c, int32_t layer) {
   return PT_OK;
 }
 
+// Whether a batch has no row: buffers of none may have no address.
+static bool no_rows(const pt_paged_batch* b) { return b->n_seqs == 0 || b->total_rows == 0; }
+
 // Checks the batch and resolves its unknown bounds.  need_ptrs: false where only sizes are asked for.
 static int check_batch(const pt_paged_cache* c, const pt_paged_batch* b, bool need_ptrs, pt_paged_rows* r) {
   if (!b) return pt_set_error(PT_ERR_NULL_POINTER, "batch is NULL");
   if (b->n_seqs < 0 || b->total_rows < 0 || b->pages_stride < 0 || b->max_q_len < 0 || b->max_kv_len < 0)
     return pt_set_error(PT_ERR_INVALID_ARGUMENT, "a size of the batch is negative");
   if (b->total_rows > (1 << 23)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "total_rows = %d exceeds 2^23", b->total_rows);
-  if (need_ptrs && b->n_seqs > 0 && b->total_rows > 0) {
+  if (need_ptrs && !no_rows(b)) {
     if (!b->row_start || !b->kv_len || (!b->pages && b->pages_stride > 0))
       return pt_set_error(PT_ERR_NULL_POINTER, "row_start, kv_len or pages is NULL");
     if (((uintptr_t)b->row_start | (uintptr_t)b->kv_len | (uintptr_t)b->pages | (uintptr_t)b->status) & 3)
@@ -75,8 +78,8 @@ static int check_batch(const pt_paged_cache* c, const pt_paged_batch* b, bool ne
   return PT_OK;
 }
 
-static int check_rows(const pt_head_rows* h, int32_t dtype, const char* name) {
-  if (!h || !h->data) return pt_set_error(PT_ERR_NULL_POINTER, "%s is NULL", name);
+static int check_rows(const pt_head_rows* h, int32_t dtype, const pt_paged_batch* b, const char* name) {
+  if (!h || (!h->data && !no_rows(b))) return pt_set_error(PT_ERR_NULL_POINTER, "%s is NULL", name);
   const int64_t vec = dtype == PT_F32 ? 4 : 8;
   if (!aligned16(h->data)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "%s is not 16-byte aligned", name);
   if (h->row_stride < 0 || h->head_stride < 0 || h->row_stride % vec || h->head_stride % vec)
@@ -123,14 +126,14 @@ extern "C" int pt_paged_append(const pt_paged_cache* cache, int32_t layer, const
   int rc = check_cache(cache);
   if (!rc) rc = check_layer(cache, layer);
   if (!rc) rc = check_batch(cache, batch, true, &a.b);
-  if (!rc) rc = check_rows(k, cache->dtype, "k");
-  if (!rc) rc = check_rows(v, cache->dtype, "v");
+  if (!rc) rc = check_rows(k, cache->dtype, batch, "k");
+  if (!rc) rc = check_rows(v, cache->dtype, batch, "v");
   if (!rc && (q != nullptr) != (q_out != nullptr)) rc = pt_set_error(PT_ERR_NULL_POINTER, "q and q_out must both be given or both be NULL");
   if (!rc && q) {
-    rc = check_rows(q, cache->dtype, "q");
-    if (!rc) rc = check_rows(q_out, cache->dtype, "q_out");
+    rc = check_rows(q, cache->dtype, batch, "q");
+    if (!rc) rc = check_rows(q_out, cache->dtype, batch, "q_out");
     if (!rc && n_heads < 1) rc = pt_set_error(PT_ERR_INVALID_ARGUMENT, "n_heads must be >= 1");
-    if (!rc && q->data == q_out->data && (q->row_stride != q_out->row_stride || q->head_stride != q_out->head_stride))
+    if (!rc && q->data && q->data == q_out->data && (q->row_stride != q_out->row_stride || q->head_stride != q_out->head_stride))
       rc = pt_set_error(PT_ERR_INVALID_ARGUMENT, "q_out is q with other strides");
   }
   if (rc) return rc;
@@ -139,7 +142,7 @@ extern "C" int pt_paged_append(const pt_paged_cache* cache, int32_t layer, const
         rope->rotary_dim > cache->head_dim)
       return pt_set_error(PT_ERR_INVALID_ARGUMENT, "the rotary description is not one of pt_rope_init for heads of %d", cache->head_dim);
   }
-  if (batch->n_seqs == 0 || batch->total_rows == 0) return PT_OK;
+  if (no_rows(batch)) return PT_OK;
   if (q) {
     a.q = q->data; a.q_rs = q->row_stride; a.q_hs = q->head_stride;
     a.q_out = q_out->data; a.qo_rs = q_out->row_stride; a.qo_hs = q_out->head_stride;
@@ -163,7 +166,7 @@ static int plan_attention(const pt_paged_cache* cache, const pt_paged_batch* bat
   if (n_heads < 1 || n_heads % cache->n_kv_heads)
     return pt_set_error(PT_ERR_INVALID_ARGUMENT, "n_kv_heads (%d) must divide n_heads (%d)", cache->n_kv_heads, n_heads);
   memset(plan, 0, sizeof(*plan));
-  if (batch->n_seqs == 0 || batch->total_rows == 0) return PT_OK;
+  if (no_rows(batch)) return PT_OK;
   return pt_plan_paged_attn(cache->dtype, cache->head_dim, n_heads, cache->n_kv_heads, *rows, plan);
 }
 
@@ -185,11 +188,11 @@ extern "C" int pt_paged_attention(const pt_paged_cache* cache, int32_t layer, co
   pt_paged_plan plan;
   int rc = plan_attention(cache, batch, n_heads, true, &a.b, &plan);
   if (!rc) rc = check_layer(cache, layer);
-  if (!rc) rc = check_rows(q, cache->dtype, "q");
-  if (!rc) rc = check_rows(out, cache->dtype, "out");
+  if (!rc) rc = check_rows(q, cache->dtype, batch, "q");
+  if (!rc) rc = check_rows(out, cache->dtype, batch, "out");
   if (rc) return rc;
   if (!isfinite(scale)) return pt_set_error(PT_ERR_INVALID_ARGUMENT, "scale is not finite");
-  if (q->data == out->data && (q->row_stride != out->row_stride || q->head_stride != out->head_stride))
+  if (q->data && q->data == out->data && (q->row_stride != out->row_stride || q->head_stride != out->head_stride))
     return pt_set_error(PT_ERR_INVALID_ARGUMENT, "out is q with other strides");
   if (plan.bytes > 0) {
     if (!workspace) return pt_set_error(PT_ERR_NULL_POINTER, "workspace is NULL, %zu bytes needed", plan.bytes);
@@ -197,7 +200,7 @@ extern "C" int pt_paged_attention(const pt_paged_cache* cache, int32_t layer, co
     if (workspace_bytes < plan.bytes)
       return pt_set_error(PT_ERR_ARENA_TOO_SMALL, "workspace: %zu bytes given, %zu needed", workspace_bytes, plan.bytes);
   }
-  if (batch->n_seqs == 0 || batch->total_rows == 0) return PT_OK;
+  if (no_rows(batch)) return PT_OK;
   a.q = q->data; a.q_rs = q->row_stride; a.q_hs = q->head_stride;
   a.o = out->data; a.o_rs = out->row_stride; a.o_hs = out->head_stride;
   a.kc = layer_of(cache->k, cache, layer);

@@ -43,3 +43,18 @@ def test_workspaces_hold_the_partials_of_rows_that_are_cut_and_no_others():
     # decode steps alone: by rows, as many as there are
     rc, n = attention_bytes(c(), batch(n_seqs=16, total_rows=16, pages_stride=8192, max_q_len=1, max_kv_len=131072), 64)
     assert rc == 0 and n == 16 * 16 * part
+
+
+def test_buffers_of_no_rows_may_have_no_address():
+    """An empty tensor has none; there is nothing to do with it."""
+    L, none = PB.lib(), PB.pt_head_rows(None, 256, 64)
+    for b in (batch(total_rows=0), batch(n_seqs=0), batch(n_seqs=0, total_rows=0, row_start=None, kv_len=None, pages=None, pages_stride=0)):
+        assert L.pt_paged_attention(cache(), 0, b, none, none, 4, 0.125, 1, None, 0, None) == 0
+        assert L.pt_paged_append(cache(), 0, b, None, none, none, 4, none, none, None) == 0
+        other = PB.pt_head_rows(None, 512, 128)               # not the same buffer
+        assert L.pt_paged_attention(cache(), 0, b, none, other, 4, 0.125, 1, None, 0, None) == 0
+        assert L.pt_paged_append(cache(), 0, b, None, none, other, 4, none, none, None) == 0
+        # the descriptors themselves are asked for all the same, and what they say has to make sense
+        assert L.pt_paged_attention(cache(), 0, b, None, none, 4, 0.125, 1, None, 0, None) == PB.PT_ERR_NULL_POINTER
+        assert L.pt_paged_attention(cache(), 0, b, PB.pt_head_rows(None, 252, 64), none, 4, 0.125, 1, None, 0, None) == BAD
+    assert L.pt_paged_attention(cache(), 0, batch(), none, none, 4, 0.125, 1, None, 0, None) == PB.PT_ERR_NULL_POINTER
