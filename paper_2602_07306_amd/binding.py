@@ -310,17 +310,19 @@ class PTPagedBatch:
         self.total_rows, self.index = total_rows, pages.get_device()
         self.c = pt_paged_batch(row_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), self.width if n <= 1 else pages.stride(0), n,
                                 total_rows, max_q_len, max_kv_len, _ptr(status))
-        self.given = max_kv_len
+        self._bound = {}   # page size: the C descriptor with its max_kv_len
 
     def bound(self, cache):
-        """The C descriptor with max_kv_len filled in from the table's width where it was not given."""
+        """The C descriptor for calls with `cache`: max_kv_len comes from the table's width where it was not given."""
         _need(self.index == cache.index, "batch and cache must be on one device")
-        room = self.width * cache.page_size
-        if self.given == 0:
-            self.c.max_kv_len = min(room, 0x7fffffff)
-        else:
-            _need(self.given <= room, "max_kv_len exceeds the page table")
-        return self.c
+        c = self._bound.get(cache.page_size)
+        if c is None:
+            room = min(self.width * cache.page_size, 0x7fffffff)
+            _need(self.c.max_kv_len <= room, "max_kv_len exceeds the page table")
+            c = pt_paged_batch.from_buffer_copy(self.c)
+            c.max_kv_len = c.max_kv_len or room
+            self._bound[cache.page_size] = c
+        return c
 
 
 def _rows(t, name: str, cache, batch, heads: int = 0):

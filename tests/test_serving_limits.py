@@ -1,6 +1,8 @@
 """What the serving operators refuse or ask for at the ends of their ranges: host logic only, no kernel is launched."""
 import ctypes as C
 
+import pytest
+
 from paper_2602_07306_amd import binding as PB
 from tests.test_serving_host import BAD, batch, cache
 
@@ -58,3 +60,18 @@ def test_buffers_of_no_rows_may_have_no_address():
         assert L.pt_paged_attention(cache(), 0, b, None, none, 4, 0.125, 1, None, 0, None) == PB.PT_ERR_NULL_POINTER
         assert L.pt_paged_attention(cache(), 0, b, PB.pt_head_rows(None, 252, 64), none, 4, 0.125, 1, None, 0, None) == BAD
     assert L.pt_paged_attention(cache(), 0, batch(), none, none, 4, 0.125, 1, None, 0, None) == PB.PT_ERR_NULL_POINTER
+
+
+def test_a_batch_used_with_two_caches_keeps_a_descriptor_for_each():
+    """The bound that follows from the table's width and the page size belongs to the call, not to the batch."""
+    torch = pytest.importorskip("torch")
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    small, large = (PB.PTPagedCache(*(torch.zeros((1, 4, 2, page, 64)) for _ in range(2))) for page in (16, 64))
+    b = PB.PTPagedBatch(i32(4), i32(3), i32(3, 4), total_rows=3)
+    first = b.bound(small)
+    second = b.bound(large)
+    assert (first.max_kv_len, second.max_kv_len, b.bound(small).max_kv_len) == (64, 256, 64)
+    given = PB.PTPagedBatch(i32(4), i32(3), i32(3, 4), total_rows=3, max_kv_len=100)
+    assert given.bound(large).max_kv_len == 100
+    with pytest.raises(PB.PTError):
+        given.bound(small)
