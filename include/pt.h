@@ -272,7 +272,8 @@ int pt_rope_init(pt_rope* out, int32_t layout, int32_t rotary_dim, double theta,
                  double high, int32_t original_len, double magnitude);
 
 /* Appends the rows' keys and values to layer `layer` of the cache, and rotates queries and keys to their rows' positions on
- * the way.  rope NULL: nothing is rotated.  k, v: rows of n_kv_heads heads.  q, q_out: rows of n_heads heads, or both NULL;
+ * the way.  rope NULL: nothing is rotated.  k, v: rows of n_kv_heads heads.  q, q_out: rows of n_heads heads (2^30 with n_kv_heads at
+ * most), or both NULL;
  * q_out may be q itself (same strides) and may not overlap it otherwise.  Rows of padding store nothing in the cache
  * (their q_out is rotated like any).  A page that receives rows must belong to one sequence of the batch only.
  * Arithmetic in fp32 on the stored values, one rounding to the dtype.

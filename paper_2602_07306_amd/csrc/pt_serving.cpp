@@ -136,6 +136,8 @@ extern "C" int pt_paged_append(const pt_paged_cache* cache, int32_t layer, const
     if (!rc && q->data && q->data == q_out->data && (q->row_stride != q_out->row_stride || q->head_stride != q_out->head_stride))
       rc = pt_set_error(PT_ERR_INVALID_ARGUMENT, "q_out is q with other strides");
   }
+  // head numbers and their sums with a workgroup's passes are 32-bit
+  if (!rc && (int64_t)(q ? n_heads : 0) + cache->n_kv_heads > 1 << 30) rc = pt_set_error(PT_ERR_INVALID_ARGUMENT, "more than 2^30 heads of queries and keys");
   if (rc) return rc;
   if (rope) {
     if ((rope->layout != PT_ROPE_HALF && rope->layout != PT_ROPE_INTERLEAVED) || rope->rotary_dim < 2 || rope->rotary_dim % 2 ||

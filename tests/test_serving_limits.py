@@ -75,3 +75,11 @@ def test_a_batch_used_with_two_caches_keeps_a_descriptor_for_each():
     assert given.bound(large).max_kv_len == 100
     with pytest.raises(PB.PTError):
         given.bound(small)
+
+
+def test_append_refuses_more_heads_than_its_numbers_hold():
+    rows = lambda at: PB.pt_head_rows(at, 256, 64)
+    append = lambda heads, **kw: PB.lib().pt_paged_append(cache(**kw), 0, batch(), None, rows(0x40000), rows(0x80000), heads, rows(0x50000), rows(0x60000), None)
+    for heads in (2 ** 31 - 1, 2 ** 30 - 1):          # beside 2 KV heads
+        assert append(heads) == BAD and "heads" in PB.pt_last_error()
+    assert append(4, n_kv_heads=2 ** 31 - 1) == BAD
