@@ -272,11 +272,10 @@ int pt_rope_init(pt_rope* out, int32_t layout, int32_t rotary_dim, double theta,
                  double high, int32_t original_len, double magnitude);
 
 /* Appends the rows' keys and values to layer `layer` of the cache, and rotates queries and keys to their rows' positions on
- * the way.  rope NULL: nothing is rotated.  k, v: rows of n_kv_heads heads.  q, q_out: rows of n_heads heads (2^30 with n_kv_heads at
- * most), or both NULL;
- * q_out may be q itself (same strides) and may not overlap it otherwise.  Rows of padding store nothing in the cache
- * (their q_out is rotated like any).  A page that receives rows must belong to one sequence of the batch only.
- * Arithmetic in fp32 on the stored values, one rounding to the dtype.
+ * the way.  rope NULL: nothing is rotated.  k, v: rows of n_kv_heads heads.  q, q_out: rows of n_heads heads, or both NULL;
+ * n_heads + n_kv_heads up to 2^30.  q_out may be q itself (same strides) and may not overlap it otherwise.  Rows of padding
+ * store nothing in the cache (their q_out is rotated like any).  A page that receives rows must belong to one sequence of
+ * the batch only.  Arithmetic in fp32 on the stored values, one rounding to the dtype.
  * Errors: NULL_POINTER, INVALID_ARGUMENT. */
 int pt_paged_append(const pt_paged_cache* cache, int32_t layer, const pt_paged_batch* batch, const pt_rope* rope,
                     const pt_head_rows* q, const pt_head_rows* q_out, int32_t n_heads, const pt_head_rows* k,
