@@ -26,3 +26,17 @@ def test_a_step_without_rows():
     assert PB.pt_sample(torch.empty((0, 100), device="cuda"), torch.empty(0, device="cuda")).shape == (0,)
     torch.cuda.synchronize()
     assert torch.all(k5 == 3.0) and torch.all(v5 == 3.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("H,Hkv,hd,lens", [(4, 2, 64, [(1, 200), (9, 40)]), (8, 1, 128, [(60, 300), (1, 700)]), (4, 2, 64, [(3, 3000), (1, 17)])])
+@pytest.mark.parametrize("factor", [30.0, 300.0])
+def test_large_scores_follow_the_definition(dtype, H, Hkv, hd, lens, factor):
+    """Scores of several hundred and thousand: the running maximum moves far, in one range and over several.  The bound of a
+    result grows with the scores, by (hd + 6) 2^-24 of their terms' sum: a few per cent of the weights here."""
+    from tests.test_gpu_paged_attention import Problem
+    p = Problem(H, Hkv, hd, dtype, 16, lens, seed=6, scale_q=factor)
+    out = p.run()
+    used = int(p.row_start[-1])
+    assert torch.isfinite(out[:used].float()).all()
+    p.check(out)
