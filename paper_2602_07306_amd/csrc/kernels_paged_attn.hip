@@ -506,9 +506,10 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
 // tiles in LDS: one that is read, one on its way).  A wavefront loads the tile's 16 keys of its number - one page - and
 // multiplies all 64 with its own rows; MFMA layouts, swizzle and transposing reads as above.  The rows' sums of probabilities
 // are one more product, with a row of ones: it costs matrix time that is free and saves as much vector time as the maximum.
-// What bounds it: 2048 rows over 16384 keys, 64 heads on 8 KV heads of 128, 1.03 TFLOP, 945 us = 1.09 PFLOP/s; matrix pipes
-// busy 51 % and vector issue 61 % of the time at 2.0 GHz.  On zeros the same call takes 851 us (the chip gives way with its
-// clock on data); without loads into LDS 840, without the exponentials 795, without LDS reads of operands 857.  Steps:
+// What bounds it: 2048 rows over 16384 keys, 64 heads on 8 KV heads of 128, 1.03 TFLOP, 930 to 975 us by the machine = 1.06 to
+// 1.11 PFLOP/s; matrix pipes busy 55 % and vector issue 54 % of the time at 2.0 GHz.  On zeros the same call takes 820 us where
+// it takes 975 (the chip gives way with its clock on data).  Of some 950: without loads into LDS 840, without the exponentials
+// 795, without LDS reads of operands 857.  Steps:
 // no overlap inside a wavefront 1058, units of 32 keys in three stages (below) 955, sums by product 940.  Measured and not
 // kept: 64 rows per wavefront, one to a SIMD (1133: scores travel between accumulation and vector registers), eight
 // wavefronts to a tile (no change), the search for the maximum spread over the second product (no change at 128, 10 %
@@ -867,7 +868,7 @@ __global__ void __launch_bounds__(256, 2) paged_attn_wide_kernel(const pt_paged_
 // Decode steps beside chunks in one launch: workgroups of the one kind wait for HBM while those of the other multiply.  Stretches
 // of 64 workgroups are dealt to the two kinds in proportion (multiples of the 8 XCDs, so that a KV head stays on its own).
 // Two workgroups share a compute unit: the few rows' tiles hold half the keys at hd = 128.  36 decode steps and 4 chunks of
-// 400 on 64 heads of 64: 179 us, one kernel behind the other 118 + 72; more of it needs more workgroups to a unit than 159
+// 400 on 64 heads of 64: 176 us, one kernel behind the other 118 + 72; more of it needs more workgroups to a unit than 159
 // registers leave (tiles of 32 keys, three workgroups: 182 to 192).
 constexpr int PA_DEAL = 64;
 template <int HD, bool FULL>

@@ -4,20 +4,24 @@
 // ones on this chip) and held as integers of 2^-S with S = 62 - ceil(log2 vocab), at most 51: sums of integers do not depend
 // on their order, so atomics, reductions and scans may run in any, and a row's answer is a function of its inputs alone.
 // The kept set of top-k and top-p is a prefix of the order (logit descending, index ascending), so it is described by
-// its last element; no filter ever sorts a row.
+// its last element, and only rows of up to SAMPLE_LIST logits are sorted whole.
 //   top-k (up to SAMPLE_LIST_K): the k-th largest of the maxima of 256 or 1024 groups of the row is a lower bound of the
 //     k-th largest logit; the few logits above it are gathered, sorted in LDS, and everything else happens among them.
-//   otherwise: a histogram of weights (or of ones) over 2048 equal steps of the logit finds the step that holds the last
-//     kept element, its members are gathered and sorted; where they do not fit, further histograms split its range of keys.
+//   top-p alone or after a larger k (sample_top_p): fp32 weights by 2048 equal steps of the logit name the step that holds the
+//     last kept element; a pass of exact weights checks that and lists the step's members, which are sorted.
+//   a larger k, and steps with more members than the list holds (sample_cut): an exact histogram of ones or weights over the
+//     steps, whose step is listed and sorted; where it does not fit, further histograms split its range of keys.
 //   pick: sixteen wavefronts sum a sixteenth of the range each, the one that holds the target is split again.
 // Rows are read from HBM once and from the caches in the later passes.
 // What bounds it: fp64 issue (about 45 instructions a weight, every compute unit on its own row) and, for top-k, a chain of
-// some fifteen steps between barriers.  256 rows of 32000 (33 MB, 6 us to read): largest logit 14 us, temperature alone 27,
-// top-k 40 24, top-k 400 45, top-p 0.95 47; one row of 32000 8.5, 19, 18, 38 and 37.
+// some fifteen steps between barriers.  256 rows of 32000 (33 MB, 6 us to read): largest logit 14 us, temperature alone 26,
+// top-k 40 24, top-k 400 45, top-p 0.95 46; one row of 32000 8.5, 19, 18, 38 and 37.
 // Few rows of many logits leave most of the chip idle and one compute unit with all fp64 work of a row: their rows are cut
 // into parts first.  sample_part_kernel finds each part's largest logit and its candidates for top-k, sample_sum_kernel each
 // wavefront's sum of weights relative to the row's largest; sample_kernel then starts from those.  The sums are the integers
-// that a row in one piece is summed by, so a row's token does not depend on how many rows the call has.
+// that a row in one piece is summed by, so a row's token does not depend on how many rows the call has.  64 rows of 130001 by
+// temperature 28 us (6.6, 13 and 8.9 in the three).  Which rows have a filter is known on the device only, so the launch of
+// sums is there for them too, and costs them 2 us: the largest logit 17 us, top-k 40 31.
 #include <algorithm>
 
 #include "pt_device.h"
@@ -494,7 +498,7 @@ __device__ __forceinline__ int sample_stretch(int n) { return ((n + 15) / 16 + 2
 // step, the sum of all, and the step's members for the list; with them the step is checked (and the next one tried), the cut is found
 // among the sorted members, and the token's stretch is known.  -2: the step holds more than the list, sample_cut finds the
 // prefix and sample_pick the token.  64 rows of 130001 logits: 240 us with sample_cut's exact histogram and
-// sample_pick, 105 so.
+// sample_pick, 109 so.
 template <typename C, typename T>
 __device__ int sample_top_p(sample_lds& s, sample_row& r, bool first, C&& cut_of, T&& target_of) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
