@@ -506,8 +506,8 @@ __global__ void __launch_bounds__(256, 1) paged_attn_kernel(const pt_paged_attn_
 // tiles in LDS: one that is read, one on its way).  A wavefront loads the tile's 16 keys of its number - one page - and
 // multiplies all 64 with its own rows; MFMA layouts, swizzle and transposing reads as above.  The rows' sums of probabilities
 // are one more product, with a row of ones: it costs matrix time that is free and saves as much vector time as the maximum.
-// What bounds it: 2048 rows over 16384 keys, 64 heads on 8 KV heads of 128, 1.03 TFLOP, 930 to 975 us by the machine = 1.06 to
-// 1.11 PFLOP/s; matrix pipes busy 55 % and vector issue 54 % of the time at 2.0 GHz.  On zeros the same call takes 820 us where
+// What bounds it: 2048 rows over 16384 keys, 64 heads on 8 KV heads of 128, 1.03 TFLOP, 910 to 975 us by the machine = 1.06 to
+// 1.13 PFLOP/s; matrix pipes busy 55 % and vector issue 54 % of the time at 2.0 GHz.  On zeros the same call takes 820 us where
 // it takes 975 (the chip gives way with its clock on data).  Of some 950: without loads into LDS 840, without the exponentials
 // 795, without LDS reads of operands 857.  Steps:
 // no overlap inside a wavefront 1058, units of 32 keys in three stages (below) 955, sums by product 940.  Measured and not
